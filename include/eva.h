@@ -498,6 +498,55 @@ size_t eva_rdecode_workspace_bytes(const eva_rcache* cache);
 int eva_generate(const eva_rcache* cache, const void* q, const void* k, const void* v, void* o, int T,
                  const int* active, void* ws, size_t ws_bytes, void* stream);
 
+/*
+ * Head norms with rotation: what stands between a layer's projection and the
+ * attention (positions as rotations, queries and keys at unit root mean
+ * square).  x holds, for every token, the heads' rows [H queries | H_kv keys | H_kv values][d] side by
+ * side; token l of sequence b starts at x + b stride_b + l stride_l (in
+ * elements; rows start on 16 bytes, strides are not negative).  One pass
+ * writes Q [B][H][L][d] and K, V [B][H_kv][L][d], what eva_prefill and, for
+ * L = 1, the append and decode calls take:
+ *     n = x g / sqrt(mean(x^2) + eps)  with g = q_weight or k_weight ([d], of
+ *                                      the tensors' type; NULL: n = x)
+ *     Q, K = n with its first `rot` features turned in pairs (a, b) ->
+ *            (a cos t - b sin t, a sin t + b cos t),  t = position * turns[i]
+ * Pair i is features (i, i + rot / 2), or (2i, 2i + 1) with interleaved = 1.
+ * The values are moved as they are.
+ *   turns    device [rot / 2]: the frequencies in 2^-64 turns per position
+ *            (2^64 theta_i / 2 pi, wrapping), so the angle of any position is
+ *            exact: a whole product modulo 2^64
+ *   rot      0 .. d, a multiple of 16 (0: no rotation, turns may be NULL)
+ *   start    device int32 [B], the position of each sequence's first token
+ *            (a ragged cache's n_tok, say); NULL: 0
+ *   offsets  device int32 [B][L], each token's distance from it (a drafted
+ *            tree's depths); NULL: 0 .. L - 1
+ * Sums are fp32, each output is rounded once.  Outputs may not overlap x.
+ * Errors: INVALID (sizes, null or misaligned pointers or rows, rot, eps not
+ * finite or below 0), UNSUPPORTED (d, dtype, L above 2^30, B L or heads beyond
+ * a grid).
+ */
+int eva_qk_norm_rope(const void* x, long long stride_b, long long stride_l, const void* q_weight, const void* k_weight,
+                     const unsigned long long* turns, int rot, int interleaved, const int* start, const int* offsets,
+                     float eps, void* Q, void* K, void* V, int B, int H, int H_kv, int L, int d, int dtype,
+                     void* stream);
+
+/*
+ * Its backward: from x and the gradients dQ [B][H][L][d], dK, dV
+ * [B][H_kv][L][d] (eva_prefill_backward's) the gradient dx of x, token-major
+ * and contiguous [B][L][H + 2 H_kv][d], and dq_weight, dk_weight (fp32 [d];
+ * looked at only where the weight is given), sums over all tokens and heads
+ * in a fixed order (no atomics: the same bits on every call).
+ * ws: device scratch of eva_qk_norm_rope_backward_workspace_bytes() bytes, not
+ * used without weights; every byte the call reads it writes first.
+ * Errors: as eva_qk_norm_rope; CAPACITY (workspace too small).
+ */
+int eva_qk_norm_rope_backward(const void* x, long long stride_b, long long stride_l, const void* q_weight,
+                              const void* k_weight, const unsigned long long* turns, int rot, int interleaved,
+                              const int* start, const int* offsets, float eps, const void* dQ, const void* dK,
+                              const void* dV, void* dx, float* dq_weight, float* dk_weight, void* ws, size_t ws_bytes,
+                              int B, int H, int H_kv, int L, int d, int dtype, void* stream);
+size_t eva_qk_norm_rope_backward_workspace_bytes(int B, int L, int d);
+
 /* Static description of an eva_status value. */
 const char* eva_status_string(int status);
 

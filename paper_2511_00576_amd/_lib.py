@@ -47,6 +47,9 @@ SYMBOLS = (
     "eva_rdecode_workspace_bytes",
     "eva_rappend_decode",
     "eva_generate",
+    "eva_qk_norm_rope",
+    "eva_qk_norm_rope_backward",
+    "eva_qk_norm_rope_backward_workspace_bytes",
     "eva_status_string",
 )
 
@@ -139,6 +142,14 @@ def load():
     lib.eva_rdecode_workspace_bytes.argtypes = [rp]
     lib.eva_generate.restype = i
     lib.eva_generate.argtypes = [rp, vp, vp, vp, vp, i, vp, vp, sz, vp]
+    ll, f = ctypes.c_longlong, ctypes.c_float
+    rope = [vp, ll, ll, vp, vp, vp, i, i, vp, vp, f]
+    lib.eva_qk_norm_rope.restype = i
+    lib.eva_qk_norm_rope.argtypes = rope + [vp, vp, vp, i, i, i, i, i, i, vp]
+    lib.eva_qk_norm_rope_backward.restype = i
+    lib.eva_qk_norm_rope_backward.argtypes = rope + [vp, vp, vp, vp, vp, vp, vp, sz, i, i, i, i, i, i, vp]
+    lib.eva_qk_norm_rope_backward_workspace_bytes.restype = sz
+    lib.eva_qk_norm_rope_backward_workspace_bytes.argtypes = [i, i, i]
     lib.eva_status_string.restype = ctypes.c_char_p
     lib.eva_status_string.argtypes = [i]
     _lib = lib

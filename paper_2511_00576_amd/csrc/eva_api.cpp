@@ -816,4 +816,98 @@ int eva_generate(const eva_rcache* cache, const void* q, const void* k, const vo
     return EVA_OK;
 }
 
+// ---------------------------------------------------------------------------
+// head norms with rotation
+// ---------------------------------------------------------------------------
+
+// Checks what the forward and the backward share and lays down its parameters.
+static int norm_rope_params(eva::NormRopeParams& p, const void* x, long long stride_b, long long stride_l,
+                            const void* q_weight, const void* k_weight, const unsigned long long* turns, int rot,
+                            int interleaved, const int* start, const int* offsets, float eps, int B, int H, int H_kv,
+                            int L, int d, int dtype) {
+    if (B < 1 || H < 1 || H_kv < 1 || L < 1) return EVA_ERR_INVALID;
+    const int st = supported(d, dtype);
+    if (st != EVA_OK) return st;
+    if (L > kMaxLen || (long long)B * L > 0x7fffffffLL - 64 || (long long)H + 2LL * H_kv > 65535)
+        return EVA_ERR_UNSUPPORTED;
+    if (!x || !aligned16(x) || !aligned16(q_weight) || !aligned16(k_weight)) return EVA_ERR_INVALID;
+    // every row starts on 16 bytes, and tokens do not overlap
+    const long long per16 = dtype == EVA_BF16 ? 8 : 4;
+    if (stride_b % per16 != 0 || stride_l % per16 != 0) return EVA_ERR_INVALID;
+    if (stride_b < 0 || stride_l < 0) return EVA_ERR_INVALID;
+    if (rot < 0 || rot > d || rot % 16 != 0 || (rot > 0 && !turns) || (interleaved != 0 && interleaved != 1))
+        return EVA_ERR_INVALID;
+    if ((reinterpret_cast<uintptr_t>(turns) & 7u) != 0) return EVA_ERR_INVALID;
+    if (!(eps >= 0.f) || eps > 1e30f) return EVA_ERR_INVALID;
+    p.x = x;
+    p.stride_b = stride_b;
+    p.stride_l = stride_l;
+    p.gq = q_weight;
+    p.gk = k_weight;
+    p.turns = turns;
+    p.start = start;
+    p.offsets = offsets;
+    p.rot = rot;
+    p.interleaved = interleaved;
+    p.eps = eps;
+    p.H = H;
+    p.Hkv = H_kv;
+    p.tokens = B * L;
+    p.fL = eva::FastDiv(L);
+    return EVA_OK;
+}
+
+int eva_qk_norm_rope(const void* x, long long stride_b, long long stride_l, const void* q_weight, const void* k_weight,
+                     const unsigned long long* turns, int rot, int interleaved, const int* start, const int* offsets,
+                     float eps, void* Q, void* K, void* V, int B, int H, int H_kv, int L, int d, int dtype,
+                     void* stream) {
+    eva::NormRopeParams p{};
+    const int st = norm_rope_params(p, x, stride_b, stride_l, q_weight, k_weight, turns, rot, interleaved, start,
+                                    offsets, eps, B, H, H_kv, L, d, dtype);
+    if (st != EVA_OK) return st;
+    if (!Q || !K || !V || !aligned16(Q) || !aligned16(K) || !aligned16(V)) return EVA_ERR_INVALID;
+    p.Q = Q;
+    p.K = K;
+    p.V = V;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return hip_status(dispatch(d, dtype, [&](auto dd, auto t) {
+        return eva::launch_norm_rope<decltype(dd)::value, decltype(t)>(p, s);
+    }));
+}
+
+size_t eva_qk_norm_rope_backward_workspace_bytes(int B, int L, int d) {
+    if (B < 1 || L < 1 || d < 1 || (long long)B * L > 0x7fffffffLL - 64) return 0;
+    return (size_t)eva::norm_rope_bwd_wgs(B * L) * 2 * d * sizeof(float);
+}
+
+int eva_qk_norm_rope_backward(const void* x, long long stride_b, long long stride_l, const void* q_weight,
+                              const void* k_weight, const unsigned long long* turns, int rot, int interleaved,
+                              const int* start, const int* offsets, float eps, const void* dQ, const void* dK,
+                              const void* dV, void* dx, float* dq_weight, float* dk_weight, void* ws, size_t ws_bytes,
+                              int B, int H, int H_kv, int L, int d, int dtype, void* stream) {
+    eva::NormRopeParams p{};
+    const int st = norm_rope_params(p, x, stride_b, stride_l, q_weight, k_weight, turns, rot, interleaved, start,
+                                    offsets, eps, B, H, H_kv, L, d, dtype);
+    if (st != EVA_OK) return st;
+    const void* must[] = {dQ, dK, dV, dx};
+    for (const void* ptr : must)
+        if (!ptr || !aligned16(ptr)) return EVA_ERR_INVALID;
+    if ((q_weight && !dq_weight) || (k_weight && !dk_weight)) return EVA_ERR_INVALID;
+    if (q_weight || k_weight) {
+        if (!ws || !aligned16(ws)) return EVA_ERR_INVALID;
+        if (ws_bytes < eva_qk_norm_rope_backward_workspace_bytes(B, L, d)) return EVA_ERR_CAPACITY;
+    }
+    p.dQ = dQ;
+    p.dK = dK;
+    p.dV = dV;
+    p.dx = dx;
+    p.dgq = q_weight ? dq_weight : nullptr;
+    p.dgk = k_weight ? dk_weight : nullptr;
+    p.ws = static_cast<float*>(ws);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return hip_status(dispatch(d, dtype, [&](auto dd, auto t) {
+        return eva::launch_norm_rope_backward<decltype(dd)::value, decltype(t)>(p, s);
+    }));
+}
+
 }  // extern "C"

@@ -251,4 +251,41 @@ hipError_t launch_decode(const DecodeParams& p, hipStream_t stream);
 constexpr size_t kDecodeScratchBytes = (size_t)6400 * 1024;
 hipError_t decode_scratch(hipStream_t stream, float** out);
 
+// Head norms with rotation (norm_rope.hip).  stride_b, stride_l: elements
+// between sequences and between tokens of x; Q, K, V and their gradients are
+// head-major and contiguous, dx is token-major and contiguous.
+struct NormRopeParams {
+    const void* x;
+    long long stride_b, stride_l;
+    const void* gq;                   // [d] or nullptr: not normalised
+    const void* gk;
+    const unsigned long long* turns;  // [rot / 2] in 2^-64 turns per position
+    const int* start;                 // [B] or nullptr: 0
+    const int* offsets;               // [B][L] or nullptr: 0 .. L - 1
+    int rot, interleaved;
+    float eps;
+    void* Q;
+    void* K;
+    void* V;
+    int H, Hkv, tokens;  // tokens = B L
+    FastDiv fL;          // divisor of L
+    // backward
+    const void* dQ;
+    const void* dK;
+    const void* dV;
+    void* dx;
+    float* dgq;  // [d]
+    float* dgk;
+    float* ws;   // [workgroups][2][d]: shares of dgq and dgk
+};
+template <int D, typename T>
+hipError_t launch_norm_rope(const NormRopeParams& p, hipStream_t stream);
+// Workgroups of the backward: every token's wave, up to four workgroups a CU.
+inline int norm_rope_bwd_wgs(int tokens) {
+    const int n = (tokens + 3) / 4;
+    return n < 1024 ? n : 1024;
+}
+template <int D, typename T>
+hipError_t launch_norm_rope_backward(const NormRopeParams& p, hipStream_t stream);
+
 }  // namespace eva

@@ -1,0 +1,306 @@
+// Norms of queries and keys per head with the position rotation, and the split
+// of the projection's output into head-major Q, K and V, in one pass; and its
+// backward.  For a token's head row x (d features) at position p:
+//
+//   n = x g / sqrt(mean(x^2) + eps)            (rows without a weight: n = x)
+//   y = n with pair i < rot / 2 turned by p turns_i:
+//       (a cos - b sin, a sin + b cos)
+//
+//   dn = the turn back of dy;  dg = sum over rows of dn x^;  x^ = x rstd
+//   dx = rstd (dn g - x^ mean(dn g x^))
+//
+// Both are bound by memory: every element is read once and written once (the
+// backward reads x and the gradients), about ten operations each.
+//
+// A row is held by D / 16 lanes of 16 features, as two 8-feature chunks that
+// hold both members of the lane's eight pairs, so a turn stays in the lane;
+// a wave works on 1024 / D rows of one token at a time and computes the
+// token's angles once for all its heads.  Angles are whole numbers: p times
+// the frequency in 2^-64 turns, modulo 2^64, is exact to 2^-64 p turns at any
+// position, where a product in fp32 is off by radians from 2^24 on.
+#include "eva_device.hpp"
+#include "eva_kernels.hpp"
+
+namespace eva {
+
+namespace {
+
+constexpr int kNormRopeWaves = 4;
+
+__device__ __forceinline__ void load8(const bf16* p, float out[8]) {
+    const u32x4 w = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        out[2 * i] = bf16_lo(w[i]);
+        out[2 * i + 1] = bf16_hi(w[i]);
+    }
+}
+__device__ __forceinline__ void load8(const float* p, float out[8]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const floatx4 w = *reinterpret_cast<const floatx4*>(p + 4 * h);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) out[4 * h + i] = w[i];
+    }
+}
+__device__ __forceinline__ void store8(bf16* p, const float x[8]) {
+    *reinterpret_cast<u32x4*>(p) = u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
+                                         pack_bf16x2(x[6], x[7])};
+}
+__device__ __forceinline__ void store8(float* p, const float x[8]) {
+    *reinterpret_cast<floatx4*>(p) = floatx4{x[0], x[1], x[2], x[3]};
+    *reinterpret_cast<floatx4*>(p + 4) = floatx4{x[4], x[5], x[6], x[7]};
+}
+
+// Where a lane's two chunks lie and how its pairs are formed.
+// ADJ: pairs are adjacent features.
+template <int D, bool ADJ>
+struct LaneRow {
+    static constexpr int kLanes = D / 16;           // lanes per row
+    static constexpr int kRows = 64 / kLanes;       // rows per wave
+    int c, sub;                                     // place in the row, row in the wave
+    int f0, f1;                                     // first feature of the chunks
+    bool turned;                                    // its pairs are turned
+    __device__ LaneRow(const NormRopeParams& a) {
+        const int lane = threadIdx.x & 63;
+        c = lane % kLanes;
+        sub = lane / kLanes;
+        turned = 16 * c < a.rot;
+        // halves: pair i is (i, i + rot / 2), so chunk c goes with chunk c + rot / 16;
+        // the features that are not turned, and adjacent pairs, lie side by side
+        const bool halves = turned && !ADJ;
+        f0 = 8 * (halves ? c : 2 * c);
+        f1 = 8 * (halves ? c + a.rot / 16 : 2 * c + 1);
+    }
+    __device__ float sum(float x) const {
+#pragma unroll
+        for (int off = 1; off < kLanes; off <<= 1) x += __shfl_xor(x, off, 64);
+        return x;
+    }
+    template <typename T>
+    __device__ void load(const T* row, float (&x)[16]) const {
+        load8(row + f0, x);
+        load8(row + f1, x + 8);
+    }
+    template <typename T>
+    __device__ void store(T* row, const float (&x)[16]) const {
+        store8(row + f0, x);
+        store8(row + f1, x + 8);
+    }
+    // SIGN 1: by the angles, -1: back
+    template <int SIGN>
+    __device__ void turn(float (&y)[16], const float (&cs)[8], const float (&sn)[8]) const {
+        if (!turned) return;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            float &lo = y[ADJ ? 2 * j : j], &hi = y[ADJ ? 2 * j + 1 : 8 + j];
+            const float p = lo, q = hi, t = SIGN * sn[j];
+            lo = p * cs[j] - q * t;
+            hi = p * t + q * cs[j];
+        }
+    }
+};
+
+// cos and sin of the lane's eight pairs at a token's position.
+template <int D, bool ADJ>
+__device__ void angles(const NormRopeParams& a, const LaneRow<D, ADJ>& r, int tok, float (&cs)[8], float (&sn)[8]) {
+    if (!r.turned) return;
+    const int b = tok / a.fL, l = tok - b * a.fL.d;
+    const long long pos = (long long)(a.start ? a.start[b] : 0) + (a.offsets ? a.offsets[tok] : l);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const unsigned long long t = (unsigned long long)pos * a.turns[8 * r.c + j];
+        // half turns in [-1, 1)
+        const float x = (float)(int)(t >> 32) * 4.656612873077393e-10f;
+        cs[j] = cospif(x);
+        sn[j] = sinpif(x);
+    }
+}
+
+// Sweeps of a token: kRows heads each, queries first, then keys, then values.
+struct Sweeps {
+    int q, k, all;
+    __device__ Sweeps(const NormRopeParams& a, int rows) {
+        q = (a.H + rows - 1) / rows;
+        const int kv = (a.Hkv + rows - 1) / rows;
+        k = q + kv;
+        all = k + kv;
+    }
+};
+
+// One wave per token (and part of its heads where there are few tokens).
+template <int D, typename T, bool ADJ>
+__global__ __launch_bounds__(kNormRopeWaves * 64) void norm_rope_kernel(NormRopeParams a) {
+    const LaneRow<D, ADJ> r(a);
+    const int tok = blockIdx.x * kNormRopeWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (tok >= a.tokens) return;
+    const int b = tok / a.fL, l = tok - b * a.fL.d;
+    const Sweeps sw(a, r.kRows);
+    const T* xt = static_cast<const T*>(a.x) + b * a.stride_b + l * a.stride_l;
+    float cs[8], sn[8];
+    angles(a, r, tok, cs, sn);
+    for (int s = blockIdx.y; s < sw.all; s += gridDim.y) {
+        if (s < sw.k) {
+            const bool key = s >= sw.q;
+            const int heads = key ? a.Hkv : a.H;
+            const int h = (key ? s - sw.q : s) * r.kRows + r.sub;
+            if (h >= heads) continue;
+            float y[16];
+            r.load(xt + (size_t)((key ? a.H : 0) + h) * D, y);
+            const T* g = static_cast<const T*>(key ? a.gk : a.gq);
+            if (g) {
+                float w[16], ss = 0.f;
+                r.load(g, w);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) ss += y[i] * y[i];
+                const float inv = rsqrtf(r.sum(ss) * (1.f / D) + a.eps);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) y[i] = y[i] * inv * w[i];
+            }
+            r.template turn<1>(y, cs, sn);
+            T* out = static_cast<T*>(key ? a.K : a.Q);
+            r.store(out + (((size_t)b * heads + h) * a.fL.d + l) * D, y);
+        } else {
+            const int h = (s - sw.k) * r.kRows + r.sub;
+            if (h >= a.Hkv) continue;
+            float y[16];
+            r.load(xt + (size_t)(a.H + a.Hkv + h) * D, y);
+            r.store(static_cast<T*>(a.V) + (((size_t)b * a.Hkv + h) * a.fL.d + l) * D, y);
+        }
+    }
+}
+
+// Tokens are dealt round to the waves; each wave's share of the weights'
+// gradients stays in registers, its workgroup's sum goes to its own place of
+// the workspace, and a second launch adds those up in their order: the same
+// bits every time.
+template <int D, typename T, bool ADJ>
+__global__ __launch_bounds__(kNormRopeWaves * 64) void norm_rope_bwd_kernel(NormRopeParams a) {
+    const LaneRow<D, ADJ> r(a);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Sweeps sw(a, r.kRows);
+    float dg[2][16] = {};
+    for (int tok = blockIdx.x * kNormRopeWaves + wave; tok < a.tokens; tok += gridDim.x * kNormRopeWaves) {
+        const int b = tok / a.fL, l = tok - b * a.fL.d;
+        const T* xt = static_cast<const T*>(a.x) + b * a.stride_b + l * a.stride_l;
+        T* dxt = static_cast<T*>(a.dx) + (size_t)tok * (a.H + 2 * a.Hkv) * D;
+        float cs[8], sn[8];
+        angles(a, r, tok, cs, sn);
+        auto rows = [&](int s, int heads, int head0, const void* grad, const void* weight, float (&acc)[16]) {
+            const int h = s * r.kRows + r.sub;
+            const bool on = h < heads;
+            const size_t row = (size_t)(head0 + min(h, heads - 1)) * D;
+            float dy[16];
+            r.load(static_cast<const T*>(grad) + (((size_t)b * heads + min(h, heads - 1)) * a.fL.d + l) * D, dy);
+            r.template turn<-1>(dy, cs, sn);
+            if (weight) {
+                float x[16], w[16], ss = 0.f;
+                r.load(xt + row, x);
+                r.load(static_cast<const T*>(weight), w);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) ss += x[i] * x[i];
+                const float inv = rsqrtf(r.sum(ss) * (1.f / D) + a.eps);
+                float dot = 0.f;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    x[i] *= inv;
+                    const float t = dy[i] * x[i];
+                    acc[i] += on ? t : 0.f;
+                    dot += t * w[i];
+                }
+                dot = r.sum(dot) * (1.f / D);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) dy[i] = inv * (dy[i] * w[i] - x[i] * dot);
+            }
+            if (on) r.store(dxt + row, dy);
+        };
+        for (int s = 0; s < sw.q; ++s) rows(s, a.H, 0, a.dQ, a.gq, dg[0]);
+        for (int s = sw.q; s < sw.k; ++s) rows(s - sw.q, a.Hkv, a.H, a.dK, a.gk, dg[1]);
+        for (int s = sw.k; s < sw.all; ++s) {
+            const int h = (s - sw.k) * r.kRows + r.sub;
+            if (h >= a.Hkv) continue;
+            float y[16];
+            r.load(static_cast<const T*>(a.dV) + (((size_t)b * a.Hkv + h) * a.fL.d + l) * D, y);
+            r.store(dxt + (size_t)(a.H + a.Hkv + h) * D, y);
+        }
+    }
+    if (!a.gq && !a.gk) return;
+    __shared__ float part[kNormRopeWaves][2][D];
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            float x = dg[n][i];
+#pragma unroll
+            for (int off = r.kLanes; off < 64; off <<= 1) x += __shfl_xor(x, off, 64);
+            if (r.sub == 0) part[wave][n][(i < 8 ? r.f0 : r.f1 - 8) + i] = x;
+        }
+    __syncthreads();
+    for (int e = threadIdx.x; e < 2 * D; e += blockDim.x) {
+        float x = 0.f;
+#pragma unroll
+        for (int w = 0; w < kNormRopeWaves; ++w) x += part[w][e / D][e % D];
+        a.ws[(size_t)blockIdx.x * 2 * D + e] = x;
+    }
+}
+
+// Sums the n workgroups' shares of 16 features: a row of 16 threads a share.
+template <int D>
+__global__ __launch_bounds__(256) void norm_rope_sum_kernel(const float* __restrict__ ws, int n, float* dgq, float* dgk) {
+    __shared__ float part[16][17];
+    const int f = threadIdx.x % 16, r = threadIdx.x / 16;
+    const int e = blockIdx.x * 16 + f;
+    float x = 0.f;
+    for (int i = r; i < n; i += 16) x += ws[(size_t)i * 2 * D + e];
+    part[r][f] = x;
+    __syncthreads();
+    if (r != 0) return;
+    x = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x += part[i][f];
+    float* out = e < D ? dgq : dgk;
+    if (out) out[e % D] = x;
+}
+
+}  // namespace
+
+template <int D, typename T>
+hipError_t launch_norm_rope(const NormRopeParams& p, hipStream_t stream) {
+    constexpr int rows = 1024 / D;
+    const int sweeps = (p.H + rows - 1) / rows + 2 * ((p.Hkv + rows - 1) / rows);
+    const int wgs = (p.tokens + kNormRopeWaves - 1) / kNormRopeWaves;
+    // few tokens: their heads over workgroups, until there are four waves a CU
+    int split = (256 + wgs - 1) / wgs;
+    if (split > sweeps) split = sweeps;
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(wgs, split), dim3(kNormRopeWaves * 64), 0, stream, p); };
+    if (p.interleaved)
+        go(norm_rope_kernel<D, T, true>);
+    else
+        go(norm_rope_kernel<D, T, false>);
+    return hipGetLastError();
+}
+
+template <int D, typename T>
+hipError_t launch_norm_rope_backward(const NormRopeParams& p, hipStream_t stream) {
+    const int wgs = norm_rope_bwd_wgs(p.tokens);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(wgs), dim3(kNormRopeWaves * 64), 0, stream, p); };
+    if (p.interleaved)
+        go(norm_rope_bwd_kernel<D, T, true>);
+    else
+        go(norm_rope_bwd_kernel<D, T, false>);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || (!p.gq && !p.gk)) return e;
+    hipLaunchKernelGGL((norm_rope_sum_kernel<D>), dim3(2 * D / 16), dim3(256), 0, stream, p.ws, wgs, p.dgq, p.dgk);
+    return hipGetLastError();
+}
+
+#define EVA_NORM_ROPE(D, T)                                                             \
+    template hipError_t launch_norm_rope<D, T>(const NormRopeParams&, hipStream_t);     \
+    template hipError_t launch_norm_rope_backward<D, T>(const NormRopeParams&, hipStream_t);
+EVA_NORM_ROPE(64, bf16)
+EVA_NORM_ROPE(128, bf16)
+EVA_NORM_ROPE(64, float)
+EVA_NORM_ROPE(128, float)
+#undef EVA_NORM_ROPE
+
+}  // namespace eva

@@ -4,6 +4,7 @@ this module only checks shapes, allocates outputs with torch and forwards
 pointers.  Tensors must live on a ROCm device; there is no CPU path.
 """
 import ctypes
+import math
 
 import torch
 
@@ -442,3 +443,106 @@ def prefill_backward(Q, K, V, Ks, Vs, O, lse, dO, W: int, C: int, workspace=None
                                            _ptr(dQ), _ptr(dK), _ptr(dV), _ptr(ws), ws.numel() * ws.element_size(), B,
                                            H, Hkv, L, d, W, C, _dtype_code(Q), window, _stream()))
     return dQ, dK, dV
+
+
+# ---- head norms with rotation ----------------------------------------------
+def _call(device, name, *args):
+    """Call lib.<name>(*args, stream) on `device`'s current stream, with that
+    device current."""
+    fn = getattr(_lib.load(), name)
+    if device.index == torch._C._cuda_getDevice():
+        _lib.check(name, fn(*args, _stream()))
+    else:
+        with torch.cuda.device(device):
+            _lib.check(name, fn(*args, _stream()))
+
+
+def _expect(t, what, shape, dtype, device):
+    """An optional operand: contiguous, of this shape and dtype, on `device`."""
+    if t is None:
+        return None
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+        raise ValueError(f"{what} must be {dtype} {list(shape)}")
+    if t.device != device:
+        raise RuntimeError(f"{what} must be on {device}")
+    if not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous")
+    return t.data_ptr()
+
+
+def rope_turns(rot: int, base: float = 10000.0, inv_freq=None, device="cuda") -> torch.Tensor:
+    """Frequencies of qk_norm_rope, int64 [rot / 2]: base^(-2i / rot), or the
+    `inv_freq` given (rot / 2 radians per position), in 2^-64 turns."""
+    if inv_freq is None:
+        inv_freq = [float(base) ** (-2.0 * i / rot) for i in range(rot // 2)]
+    inv_freq = [float(f) for f in inv_freq]
+    if len(inv_freq) != rot // 2:
+        raise ValueError("inv_freq must hold rot / 2 frequencies")
+    t = [round(f / (2 * math.pi) * 2 ** 64) % 2 ** 64 for f in inv_freq]
+    return torch.tensor([x - 2 ** 64 if x >= 2 ** 63 else x for x in t], dtype=torch.int64, device=device)
+
+
+def _norm_rope_args(x, H, Hkv, turns, q_weight, k_weight, eps, start, offsets, interleaved):
+    """The arguments both directions share, and (B, L, d)."""
+    if not x.is_cuda:
+        raise RuntimeError("EVA kernels run on the GPU only: tensors must be on a ROCm device")
+    if x.dim() != 3 or H < 1 or Hkv < 1 or x.shape[2] % (H + 2 * Hkv) != 0:
+        raise ValueError("x must be [B, L, (H + 2 Hkv) * d]")
+    if x.stride(2) != 1:
+        raise ValueError("the features of x must be contiguous")
+    B, L, d = x.shape[0], x.shape[1], x.shape[2] // (H + 2 * Hkv)
+    # the stride of a single row is never used, and may be any number
+    sb, sl = x.stride(0) if B > 1 else 0, x.stride(1) if L > 1 else 0
+    rot = 0 if turns is None else 2 * turns.numel()
+    return (_ptr(x), sb, sl, _expect(q_weight, "q_weight", (d,), x.dtype, x.device),
+            _expect(k_weight, "k_weight", (d,), x.dtype, x.device),
+            _expect(turns, "turns", (rot // 2,), torch.int64, x.device), rot, int(bool(interleaved)),
+            _expect(start, "start", (B,), torch.int32, x.device),
+            _expect(offsets, "offsets", (B, L), torch.int32, x.device), float(eps)), B, L, d
+
+
+def qk_norm_rope(x, H: int, Hkv: int, turns=None, q_weight=None, k_weight=None, eps: float = 1e-6, start=None,
+                 offsets=None, interleaved: bool = False, out=None):
+    """Head norms with rotation: x [B, L, (H + 2 Hkv) * d], a projection's
+    output (its rows may be strided), -> Q [B, H, L, d], K, V [B, Hkv, L, d].
+
+    `q_weight`, `k_weight` [d]: weights of the root-mean-square norms (None:
+    no norm).  `turns`: rope_turns' frequencies (None: no rotation).  The
+    token's position is start[b] (int32 [B], a ragged cache's n_tok for one;
+    None: 0) + offsets[b, l] (int32 [B, L]; None: l).  `out` = (Q, K, V)
+    preallocated."""
+    args, B, L, d = _norm_rope_args(x, H, Hkv, turns, q_weight, k_weight, eps, start, offsets, interleaved)
+    if out is None:
+        Q = torch.empty(B, H, L, d, dtype=x.dtype, device=x.device)
+        K, V = (torch.empty(B, Hkv, L, d, dtype=x.dtype, device=x.device) for _ in range(2))
+    else:
+        Q, K, V = out
+    if B == 0 or L == 0:
+        return Q, K, V
+    _call(x.device, "eva_qk_norm_rope", *args, _expect(Q, "Q", (B, H, L, d), x.dtype, x.device),
+          _expect(K, "K", (B, Hkv, L, d), x.dtype, x.device), _expect(V, "V", (B, Hkv, L, d), x.dtype, x.device), B, H,
+          Hkv, L, d, _dtype_code(x))
+    return Q, K, V
+
+
+def qk_norm_rope_backward(x, dQ, dK, dV, turns=None, q_weight=None, k_weight=None, eps: float = 1e-6, start=None,
+                          offsets=None, interleaved: bool = False):
+    """Gradients of qk_norm_rope: dQ [B, H, L, d], dK, dV [B, Hkv, L, d] ->
+    (dx [B, L, (H + 2 Hkv) * d], dq_weight, dk_weight), the weights' in fp32
+    (None where there is no weight)."""
+    H, Hkv = dQ.shape[1], dK.shape[1]
+    args, B, L, d = _norm_rope_args(x, H, Hkv, turns, q_weight, k_weight, eps, start, offsets, interleaved)
+    grads = (_expect(dQ, "dQ", (B, H, L, d), x.dtype, x.device), _expect(dK, "dK", (B, Hkv, L, d), x.dtype, x.device),
+             _expect(dV, "dV", (B, Hkv, L, d), x.dtype, x.device))
+    dx = torch.empty(B, L, x.shape[2], dtype=x.dtype, device=x.device)
+    new = torch.zeros if B == 0 or L == 0 else torch.empty
+    dg = [None if w is None else new(d, dtype=torch.float32, device=x.device) for w in (q_weight, k_weight)]
+    if B == 0 or L == 0:
+        return (dx, *dg)
+    ws = None
+    if q_weight is not None or k_weight is not None:
+        n = _lib.load().eva_qk_norm_rope_backward_workspace_bytes(B, L, d)
+        ws = torch.empty((n + 3) // 4, dtype=torch.float32, device=x.device)
+    _call(x.device, "eva_qk_norm_rope_backward", *args, *grads, _ptr(dx), _ptr(dg[0]), _ptr(dg[1]), _ptr(ws),
+          ws.numel() * 4 if ws is not None else 0, B, H, Hkv, L, d, _dtype_code(x))
+    return (dx, *dg)
