@@ -547,6 +547,121 @@ int eva_qk_norm_rope_backward(const void* x, long long stride_b, long long strid
                               int B, int H, int H_kv, int L, int d, int dtype, void* stream);
 size_t eva_qk_norm_rope_backward_workspace_bytes(int B, int L, int d);
 
+/*
+ * Drafted tokens (speculative generation): a small model proposes a tree of
+ * tokens for every sequence, the model's own attention rows of all of them
+ * are computed at once, and the tokens of the path that is accepted are
+ * appended.
+ *
+ * eva_rtree_attention: q, o [B][H][T][d]; k, v [B][H_kv][T][d], the drafted
+ * tokens' rows, in the cache's dtype.  parents is device int32 [B][T]: the
+ * node that node t continues, an earlier one (parents[t] < t); any other value
+ * makes t a root, which continues the sequence itself.  n_nodes (device int32
+ * [B], clamped to 0 .. T; NULL: T) is each tree's size.  Node t stands at
+ * position p = n_tok[b] + its depth, and o[b][:][t] is its row: the softmax
+ * over the ring's window positions below n_tok[b], the summaries c < s(p) and
+ * the keys of the node itself and of the nodes it continues.  A chain
+ * (parents[t] = t - 1) gives the rows that T steps of eva_rappend_decode would
+ * give (summaries of chunks that the drafted tokens complete are not visible
+ * within W steps).  Rows of inactive sequences and of nodes that there are not
+ * are left as they were; the cache is not changed.
+ * T is at most 64 and at most W, so that no drafted token leaves a window or
+ * enters a visible summary; a cache of EVA_WINDOW_BLOCKED takes T = 1 alone.
+ * ws: optional device scratch, as in eva_rdecode_step, of
+ * eva_rtree_workspace_bytes(cache, T) bytes.
+ * Errors: INVALID (malformed cache, T < 1 or > W, null or misaligned q, k, v, o,
+ * parents), UNSUPPORTED (T > 64, blocked window with T > 1, grids).
+ */
+int eva_rtree_attention(const eva_rcache* cache, const void* q, const void* k, const void* v, const int* parents,
+                        const int* n_nodes, void* o, int T, const int* active, void* ws, size_t ws_bytes, void* stream);
+size_t eva_rtree_workspace_bytes(const eva_rcache* cache, int T);
+
+/*
+ * Append a path of drafted tokens to every active sequence: the tokens
+ * k[b][:][path[b][i]], v likewise, for i < counts[b], in this order, as
+ * eva_rcache_append would one by one (the chunks they complete are summarised,
+ * the same bits).
+ *   path    device int32 [B][T], or NULL: 0, 1, ...  The first entry outside
+ *           0 .. T - 1 ends a sequence's path.
+ *   counts  device int32 [B], clamped to 0 .. T, or NULL: T
+ * A sequence that becomes full takes no more tokens.  T as in
+ * eva_rtree_attention (any causal window).
+ * Errors: INVALID (malformed cache, T < 1 or > W, null or misaligned k, v),
+ * UNSUPPORTED (T > 64).
+ */
+int eva_rappend_path(const eva_rcache* cache, const void* k, const void* v, const int* path, const int* counts, int T,
+                     const int* active, void* stream);
+
+/*
+ * 8-bit decode cache: a ragged cache (eva_rcache) of rows in e4m3 (the OCP
+ * format of 4 exponent and 3 mantissa bits, largest value 448) with a
+ * power of two for each row, half the bytes of a bf16 one.  A row x is held as
+ * d codes and one byte e:
+ *     x_i ~ code_i 2^(e - 127),  code_i = e4m3(x_i 2^(127 - e)) (ties to even),
+ * e the smallest that brings the row's largest finite magnitude to 448 or
+ * below (127 for a row of zeros; 1 .. 246).  So every entry above 2^-15 of the
+ * row's largest is off by 2^-4 of itself at most.  Entries that are not finite
+ * are held as NaN.  q, k, v, o are bf16.
+ *   k_ring  [B][H_kv][R][d]            codes, row per slot
+ *   vt_ring [B][H_kv][R/16][d][16]     codes: slot s, feature f at [s/16][f][s%16]
+ *   k_sum   [B][H_kv][S_max][d]
+ *   vt_sum  [B][H_kv][S_max/16][d][16]
+ *   *_exp   [B][H_kv][R] and [B][H_kv][S_max]: the rows' bytes e
+ * All eight 16-byte aligned.  Requirements: R >= W + C - 1; R and S_max
+ * multiples of 64; S_max >= max_tok / C.  n_tok, arrive, max_tok as in
+ * eva_rcache.  Summaries are the deterministic ones.
+ */
+typedef struct eva_qcache {
+    int B, H, H_kv, d, W, C;
+    int window;       /* eva_window, causal */
+    int R;
+    int S_max;
+    int max_tok;
+    int* n_tok;
+    int* arrive;
+    void* k_ring;
+    void* vt_ring;
+    void* k_sum;
+    void* vt_sum;
+    unsigned char* k_ring_exp;
+    unsigned char* v_ring_exp;
+    unsigned char* k_sum_exp;
+    unsigned char* v_sum_exp;
+} eva_qcache;
+
+/* eva_rcache_fill into an 8-bit cache (K, V, Ksum, Vsum bf16). */
+int eva_qcache_fill(const eva_qcache* cache, const void* K, const void* V, const void* Ksum, const void* Vsum, int L,
+                    const int* lens, void* stream);
+
+/* eva_rcache_append and eva_rappend_path into an 8-bit cache (k_new, v_new
+ * 16-byte aligned).  The summary of a chunk that is completed is built from
+ * the chunk's rows as the cache holds them, and quantised in its turn. */
+int eva_qcache_append(const eva_qcache* cache, const void* k_new, const void* v_new, const int* active, void* stream);
+int eva_qappend_path(const eva_qcache* cache, const void* k, const void* v, const int* path, const int* counts, int T,
+                     const int* active, void* stream);
+
+/* Copy the rows of an 8-bit cache into a bf16 ragged cache of the same B, H,
+ * H_kv, d, W, C and window (rf = 0), whose sequences then go on from there: the
+ * last positions that both rings hold, the summaries, the token counts.  The
+ * values are exact in bf16 (below 2^-126: to its subnormals).  Slots that hold
+ * no row are left as they were.
+ * Errors: INVALID (malformed or different caches), UNSUPPORTED (an fp32 one),
+ * CAPACITY (its max_tok below this one's). */
+int eva_qcache_read(const eva_qcache* cache, const eva_rcache* to, void* stream);
+
+/* eva_rdecode_step, eva_rappend_decode (the append, then the decode: the row
+ * reads its own token as the cache holds it) and eva_rtree_attention (drafted
+ * tokens are read as they are given, in bf16) over an 8-bit cache; q and o
+ * 16-byte aligned. */
+int eva_qdecode_step(const eva_qcache* cache, const void* q, void* o, const int* active, void* ws, size_t ws_bytes,
+                     void* stream);
+size_t eva_qdecode_workspace_bytes(const eva_qcache* cache);
+int eva_qappend_decode(const eva_qcache* cache, const void* q, const void* k_new, const void* v_new, void* o,
+                       const int* active, void* ws, size_t ws_bytes, void* stream);
+int eva_qtree_attention(const eva_qcache* cache, const void* q, const void* k, const void* v, const int* parents,
+                        const int* n_nodes, void* o, int T, const int* active, void* ws, size_t ws_bytes, void* stream);
+size_t eva_qtree_workspace_bytes(const eva_qcache* cache, int T);
+
 /* Static description of an eva_status value. */
 const char* eva_status_string(int status);
 

@@ -50,6 +50,18 @@ SYMBOLS = (
     "eva_qk_norm_rope",
     "eva_qk_norm_rope_backward",
     "eva_qk_norm_rope_backward_workspace_bytes",
+    "eva_rtree_attention",
+    "eva_rtree_workspace_bytes",
+    "eva_rappend_path",
+    "eva_qcache_fill",
+    "eva_qcache_append",
+    "eva_qappend_path",
+    "eva_qcache_read",
+    "eva_qdecode_step",
+    "eva_qdecode_workspace_bytes",
+    "eva_qappend_decode",
+    "eva_qtree_attention",
+    "eva_qtree_workspace_bytes",
     "eva_status_string",
 )
 
@@ -74,6 +86,19 @@ class EvaRCacheStruct(ctypes.Structure):
         ("k_ring", ctypes.c_void_p), ("vt_ring", ctypes.c_void_p),
         ("k_sum", ctypes.c_void_p), ("vt_sum", ctypes.c_void_p),
         ("rf", ctypes.c_int), ("rf_lambda", ctypes.c_float), ("rf_seed", ctypes.c_ulonglong),
+    ]
+
+
+class EvaQCacheStruct(ctypes.Structure):
+    _fields_ = [
+        ("B", ctypes.c_int), ("H", ctypes.c_int), ("H_kv", ctypes.c_int), ("d", ctypes.c_int),
+        ("W", ctypes.c_int), ("C", ctypes.c_int), ("window", ctypes.c_int),
+        ("R", ctypes.c_int), ("S_max", ctypes.c_int), ("max_tok", ctypes.c_int),
+        ("n_tok", ctypes.c_void_p), ("arrive", ctypes.c_void_p),
+        ("k_ring", ctypes.c_void_p), ("vt_ring", ctypes.c_void_p),
+        ("k_sum", ctypes.c_void_p), ("vt_sum", ctypes.c_void_p),
+        ("k_ring_exp", ctypes.c_void_p), ("v_ring_exp", ctypes.c_void_p),
+        ("k_sum_exp", ctypes.c_void_p), ("v_sum_exp", ctypes.c_void_p),
     ]
 
 
@@ -150,6 +175,26 @@ def load():
     lib.eva_qk_norm_rope_backward.argtypes = rope + [vp, vp, vp, vp, vp, vp, vp, sz, i, i, i, i, i, i, vp]
     lib.eva_qk_norm_rope_backward_workspace_bytes.restype = sz
     lib.eva_qk_norm_rope_backward_workspace_bytes.argtypes = [i, i, i]
+    qp = ctypes.POINTER(EvaQCacheStruct)
+    for cache, p in ((rp, "eva_r"), (qp, "eva_q")):
+        getattr(lib, p + "tree_attention").restype = i
+        getattr(lib, p + "tree_attention").argtypes = [cache, vp, vp, vp, vp, vp, vp, i, vp, vp, sz, vp]
+        getattr(lib, p + "tree_workspace_bytes").restype = sz
+        getattr(lib, p + "tree_workspace_bytes").argtypes = [cache, i]
+        getattr(lib, p + "append_path").restype = i
+        getattr(lib, p + "append_path").argtypes = [cache, vp, vp, vp, vp, i, vp, vp]
+    lib.eva_qcache_fill.restype = i
+    lib.eva_qcache_fill.argtypes = [qp, vp, vp, vp, vp, i, vp, vp]
+    lib.eva_qcache_append.restype = i
+    lib.eva_qcache_append.argtypes = [qp, vp, vp, vp, vp]
+    lib.eva_qcache_read.restype = i
+    lib.eva_qcache_read.argtypes = [qp, rp, vp]
+    lib.eva_qdecode_step.restype = i
+    lib.eva_qdecode_step.argtypes = [qp, vp, vp, vp, vp, sz, vp]
+    lib.eva_qdecode_workspace_bytes.restype = sz
+    lib.eva_qdecode_workspace_bytes.argtypes = [qp]
+    lib.eva_qappend_decode.restype = i
+    lib.eva_qappend_decode.argtypes = [qp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.eva_status_string.restype = ctypes.c_char_p
     lib.eva_status_string.argtypes = [i]
     _lib = lib

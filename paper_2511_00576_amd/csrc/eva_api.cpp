@@ -910,4 +910,298 @@ int eva_qk_norm_rope_backward(const void* x, long long stride_b, long long strid
     }));
 }
 
+// ---------------------------------------------------------------------------
+// 8-bit cache, drafted trees
+// ---------------------------------------------------------------------------
+
+namespace {
+
+int check_qcache(const eva_qcache* c) {
+    if (!c) return EVA_ERR_INVALID;
+    if (c->B < 1 || c->H < 1 || c->H_kv < 1 || c->H % c->H_kv != 0 || c->W < 1 || c->C < 1 || c->C > kMaxChunk)
+        return EVA_ERR_INVALID;
+    const int st = supported(c->d, EVA_BF16);
+    if (st != EVA_OK) return st;
+    const void* must[] = {c->k_ring, c->vt_ring, c->k_sum, c->vt_sum, c->k_ring_exp, c->v_ring_exp, c->k_sum_exp, c->v_sum_exp};
+    for (const void* ptr : must)
+        if (!ptr || !aligned16(ptr)) return EVA_ERR_INVALID;
+    if (!c->n_tok || !c->arrive || c->max_tok < 1) return EVA_ERR_INVALID;
+    if (c->max_tok > kMaxLen) return EVA_ERR_UNSUPPORTED;
+    if (!valid_window(c->window) || c->window == EVA_WINDOW_NONCAUSAL) return EVA_ERR_INVALID;
+    if (c->R < 64 || c->R % 64 != 0 || c->S_max < 64 || c->S_max % 64 != 0) return EVA_ERR_INVALID;
+    if ((long long)c->R < (long long)c->W + c->C - 1) return EVA_ERR_CAPACITY;
+    if (c->max_tok / c->C > c->S_max) return EVA_ERR_CAPACITY;
+    if ((long long)c->B * c->H_kv > 65535) return EVA_ERR_UNSUPPORTED;
+    return EVA_OK;
+}
+
+eva::QCacheView qview_of(const eva_qcache* c) {
+    eva::QCacheView v;
+    v.B = c->B;
+    v.H = c->H;
+    v.Hkv = c->H_kv;
+    v.W = c->W;
+    v.C = c->C;
+    v.R = c->R;
+    v.S_max = c->S_max;
+    v.window = c->window;
+    v.k_ring = static_cast<uint8_t*>(c->k_ring);
+    v.vt_ring = static_cast<uint8_t*>(c->vt_ring);
+    v.k_sum = static_cast<uint8_t*>(c->k_sum);
+    v.vt_sum = static_cast<uint8_t*>(c->vt_sum);
+    v.k_ring_e = c->k_ring_exp;
+    v.v_ring_e = c->v_ring_exp;
+    v.k_sum_e = c->k_sum_exp;
+    v.v_sum_e = c->v_sum_exp;
+    return v;
+}
+// The geometry of an 8-bit cache where a kernel takes any cache's.
+eva::CacheView qgeometry_of(const eva_qcache* c) {
+    eva::CacheView v{};
+    v.B = c->B;
+    v.H = c->H;
+    v.Hkv = c->H_kv;
+    v.W = c->W;
+    v.C = c->C;
+    v.R = c->R;
+    v.S_max = c->S_max;
+    v.window = c->window;
+    return v;
+}
+
+// Longest drafted tree, or accepted path, of one call.
+int check_nodes(int T, int W) {
+    if (T < 1 || T > W) return EVA_ERR_INVALID;
+    return T > eva::kMaxPath ? EVA_ERR_UNSUPPORTED : EVA_OK;
+}
+
+// Most chunks of `keys` keys that a row of a sequence of max_tok tokens touches.
+int row_chunks(int window, int max_tok, int W, int C, int S_max, int keys) {
+    int n_sum = prefix_summaries(window, max_tok, W, C);
+    if (n_sum > S_max) n_sum = S_max;
+    const long long w = window == EVA_WINDOW_CHUNK_ALIGNED ? (long long)W + C - 1 : W;
+    const int win = (int)(w < max_tok ? w : max_tok);
+    return (n_sum + keys - 1) / keys + (win + keys - 2) / keys + 1;
+}
+
+// How the query columns of a kv head and its keys are laid over workgroups: what
+// a launch does and what the workspace queries answer.
+struct TreeRoute {
+    int shape, col_blocks, splits;
+    size_t ws_bytes;
+};
+TreeRoute tree_route(long long units, long long cols, int d, int dtype, bool drafted, int n_chunks) {
+    TreeRoute r;
+    r.shape = eva::kTreeNarrow;
+    if (dtype == EVA_BF16 && drafted)
+        r.shape = cols <= 16 ? eva::kTreeNarrow : cols <= 32 ? eva::kTree32 : cols <= 64 ? eva::kTree64 : eva::kTree128;
+    const int per = eva::tree_shape_cols(r.shape);
+    const long long blocks = (cols + per - 1) / per, wgs = units * blocks;
+    r.col_blocks = (int)blocks;
+    if (r.shape == eva::kTreeNarrow && wgs < 256 && n_chunks > 4 && n_chunks <= 20) r.shape = eva::kTreeNarrowWide;
+    const int kw = eva::tree_shape_key_waves(r.shape);
+    r.splits = 1;
+    if (r.shape != eva::kTreeNarrowWide && wgs < 256) {
+        long long s = (512 + wgs - 1) / wgs;
+        const long long most = (n_chunks + kw - 1) / kw;
+        r.splits = (int)(s > most ? most : s);
+    }
+    r.ws_bytes = r.splits > 1 ? (size_t)units * r.splits * cols * (d + 2) * sizeof(float) : 0;
+    return r;
+}
+
+// Parameters that every kind of cache shares; q and o of `per` rows a head.
+int tree_params(eva::TreeParams& p, TreeRoute& r, const eva::CacheView& v, int d, int dtype, const int* n_tok, int max_tok,
+                const int* active, const void* q, void* o, int T, bool drafted, int n_chunks, void* ws, size_t ws_bytes) {
+    if (!q || !o || !aligned16(q) || !aligned16(o)) return EVA_ERR_INVALID;
+    const long long units = (long long)v.B * v.Hkv, cols = (long long)(v.H / v.Hkv) * T;
+    if (cols > 0x7fffffffLL / 128) return EVA_ERR_UNSUPPORTED;
+    r = tree_route(units, cols, d, dtype, drafted, n_chunks);
+    if ((units + 7) / 8 * 8 * r.col_blocks > 0x7fffffffLL || r.col_blocks > (1 << 27)) return EVA_ERR_UNSUPPORTED;
+    p.c = v;
+    p.n_tok = n_tok;
+    p.active = active;
+    p.max_tok = max_tok;
+    p.q = q;
+    p.o = o;
+    p.T = T;
+    p.G = v.H / v.Hkv;
+    p.cols = (int)cols;
+    p.fT = eva::FastDiv(T);
+    p.col_blocks = r.col_blocks;
+    p.units = (int)units;
+    p.f8cb = eva::FastDiv(8 * r.col_blocks);
+    p.fHkv = eva::FastDiv(v.Hkv);
+    p.splits = r.splits > 1 && ws && aligned16(ws) && ws_bytes >= r.ws_bytes ? r.splits : 1;
+    p.ws = p.splits > 1 ? static_cast<float*>(ws) : nullptr;
+    p.scale_log2 = (float)(1.4426950408889634 / sqrt((double)d));
+    p.log2C = (float)log2((double)v.C);
+    p.shape = r.shape;
+    return EVA_OK;
+}
+
+// The tree's own operands.
+int tree_nodes(eva::TreeParams& p, const void* k, const void* v, const int* parents, const int* n_nodes, int T, int W, int window) {
+    const int st = check_nodes(T, W);
+    if (st != EVA_OK) return st;
+    if (!k || !v || !parents || !aligned16(k) || !aligned16(v)) return EVA_ERR_INVALID;
+    // a blocked window's next block would need summaries of drafted tokens
+    if (window == EVA_WINDOW_BLOCKED && T > 1) return EVA_ERR_UNSUPPORTED;
+    p.k = k;
+    p.v = v;
+    p.parents = parents;
+    p.n_nodes = n_nodes;
+    return EVA_OK;
+}
+
+int r_chunks(const eva_rcache* c) { return row_chunks(c->window, c->max_tok, c->W, c->C, c->S_max, 32); }
+int q_chunks(const eva_qcache* c) { return row_chunks(c->window, c->max_tok, c->W, c->C, c->S_max, 64); }
+
+int launch_q(const eva::TreeParams& p, int d, void* stream) {
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return hip_status(d == 64 ? eva::launch_tree<64, true>(p, s) : eva::launch_tree<128, true>(p, s));
+}
+
+eva::PathParams path_params(const void* k, const void* v, const int* path, const int* counts, int T, int* n_tok, int* arrive,
+                            const int* active, int max_tok) {
+    return eva::PathParams{k, v, path, counts, T, n_tok, arrive, active, max_tok};
+}
+
+}  // namespace
+
+size_t eva_rtree_workspace_bytes(const eva_rcache* cache, int T) {
+    if (check_rcache(cache) != EVA_OK || check_nodes(T, cache->W) != EVA_OK) return 0;
+    const long long cols = (long long)(cache->H / cache->H_kv) * T;
+    return tree_route((long long)cache->B * cache->H_kv, cols, cache->d, cache->dtype, true, r_chunks(cache) + (T + 31) / 32).ws_bytes;
+}
+
+int eva_rtree_attention(const eva_rcache* cache, const void* q, const void* k, const void* v, const int* parents,
+                        const int* n_nodes, void* o, int T, const int* active, void* ws, size_t ws_bytes, void* stream) {
+    int st = check_rcache(cache);
+    if (st != EVA_OK) return st;
+    eva::TreeParams p{};
+    st = tree_nodes(p, k, v, parents, n_nodes, T, cache->W, cache->window);
+    if (st != EVA_OK) return st;
+    TreeRoute r;
+    st = tree_params(p, r, rview_of(cache), cache->d, cache->dtype, cache->n_tok, cache->max_tok, active, q, o, T, true,
+                     r_chunks(cache) + (T + 31) / 32, ws, ws_bytes);
+    if (st != EVA_OK) return st;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (cache->dtype == EVA_F32)
+        return hip_status(cache->d == 64 ? eva::launch_tree_f32<64>(p, s) : eva::launch_tree_f32<128>(p, s));
+    return hip_status(cache->d == 64 ? eva::launch_tree<64, false>(p, s) : eva::launch_tree<128, false>(p, s));
+}
+
+int eva_rappend_path(const eva_rcache* cache, const void* k, const void* v, const int* path, const int* counts, int T,
+                     const int* active, void* stream) {
+    int st = check_rcache(cache);
+    if (st != EVA_OK) return st;
+    st = check_nodes(T, cache->W);
+    if (st != EVA_OK) return st;
+    if (!k || !v || !aligned16(k) || !aligned16(v)) return EVA_ERR_INVALID;
+    const eva::CacheView view = rview_of(cache);
+    const eva::PathParams a = path_params(k, v, path, counts, T, cache->n_tok, cache->arrive, active, cache->max_tok);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return hip_status(dispatch(cache->d, cache->dtype, [&](auto dd, auto t) {
+        return eva::launch_append_path<decltype(dd)::value, decltype(t)>(view, a, s);
+    }));
+}
+
+int eva_qcache_fill(const eva_qcache* cache, const void* K, const void* V, const void* Ksum, const void* Vsum, int L,
+                    const int* lens, void* stream) {
+    int st = check_qcache(cache);
+    if (st != EVA_OK) return st;
+    if (L < 1 || !K || !V || !lens || !aligned16(K) || !aligned16(V)) return EVA_ERR_INVALID;
+    if (L > kMaxLen) return EVA_ERR_UNSUPPORTED;
+    const int n_chunks = L / cache->C;
+    if (n_chunks > 0 && (!Ksum || !Vsum || !aligned16(Ksum) || !aligned16(Vsum))) return EVA_ERR_INVALID;
+    if (cache->S_max < (L < cache->max_tok ? L : cache->max_tok) / cache->C) return EVA_ERR_CAPACITY;
+    const eva::RaggedState r{cache->n_tok, cache->arrive, nullptr, cache->max_tok};
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const eva::QCacheView v = qview_of(cache);
+    return hip_status(cache->d == 64 ? eva::launch_qcache_fill<64>(v, K, V, Ksum, Vsum, L, lens, r, s)
+                                     : eva::launch_qcache_fill<128>(v, K, V, Ksum, Vsum, L, lens, r, s));
+}
+
+int eva_qappend_path(const eva_qcache* cache, const void* k, const void* v, const int* path, const int* counts, int T,
+                     const int* active, void* stream) {
+    int st = check_qcache(cache);
+    if (st != EVA_OK) return st;
+    st = check_nodes(T, cache->W);
+    if (st != EVA_OK) return st;
+    if (!k || !v || !aligned16(k) || !aligned16(v)) return EVA_ERR_INVALID;
+    const eva::PathParams a = path_params(k, v, path, counts, T, cache->n_tok, cache->arrive, active, cache->max_tok);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return hip_status(cache->d == 64 ? eva::launch_qappend_path<64>(qview_of(cache), a, s)
+                                     : eva::launch_qappend_path<128>(qview_of(cache), a, s));
+}
+
+int eva_qcache_append(const eva_qcache* cache, const void* k_new, const void* v_new, const int* active, void* stream) {
+    return eva_qappend_path(cache, k_new, v_new, nullptr, nullptr, 1, active, stream);
+}
+
+int eva_qcache_read(const eva_qcache* cache, const eva_rcache* to, void* stream) {
+    int st = check_qcache(cache);
+    if (st != EVA_OK) return st;
+    st = check_rcache(to);
+    if (st != EVA_OK) return st;
+    if (to->dtype != EVA_BF16) return EVA_ERR_UNSUPPORTED;
+    if (to->B != cache->B || to->H != cache->H || to->H_kv != cache->H_kv || to->d != cache->d || to->W != cache->W ||
+        to->C != cache->C || to->window != cache->window || to->rf != 0)
+        return EVA_ERR_INVALID;
+    if (to->max_tok < cache->max_tok) return EVA_ERR_CAPACITY;
+    const eva::RaggedState r = rstate_of(to, nullptr);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return hip_status(cache->d == 64
+                          ? eva::launch_qcache_read<64>(qview_of(cache), rview_of(to), cache->n_tok, cache->max_tok, r, s)
+                          : eva::launch_qcache_read<128>(qview_of(cache), rview_of(to), cache->n_tok, cache->max_tok, r, s));
+}
+
+size_t eva_qdecode_workspace_bytes(const eva_qcache* cache) {
+    if (check_qcache(cache) != EVA_OK) return 0;
+    return tree_route((long long)cache->B * cache->H_kv, cache->H / cache->H_kv, cache->d, EVA_BF16, false, q_chunks(cache)).ws_bytes;
+}
+
+int eva_qdecode_step(const eva_qcache* cache, const void* q, void* o, const int* active, void* ws, size_t ws_bytes,
+                     void* stream) {
+    int st = check_qcache(cache);
+    if (st != EVA_OK) return st;
+    eva::TreeParams p{};
+    p.qc = qview_of(cache);
+    TreeRoute r;
+    st = tree_params(p, r, qgeometry_of(cache), cache->d, EVA_BF16, cache->n_tok, cache->max_tok, active, q, o, 1, false,
+                     q_chunks(cache), ws, ws_bytes);
+    if (st != EVA_OK) return st;
+    return launch_q(p, cache->d, stream);
+}
+
+int eva_qappend_decode(const eva_qcache* cache, const void* q, const void* k_new, const void* v_new, void* o,
+                       const int* active, void* ws, size_t ws_bytes, void* stream) {
+    if (!q || !o || !aligned16(q) || !aligned16(o)) return EVA_ERR_INVALID;
+    const int st = eva_qcache_append(cache, k_new, v_new, active, stream);
+    if (st != EVA_OK) return st;
+    return eva_qdecode_step(cache, q, o, active, ws, ws_bytes, stream);
+}
+
+size_t eva_qtree_workspace_bytes(const eva_qcache* cache, int T) {
+    if (check_qcache(cache) != EVA_OK || check_nodes(T, cache->W) != EVA_OK) return 0;
+    const long long cols = (long long)(cache->H / cache->H_kv) * T;
+    return tree_route((long long)cache->B * cache->H_kv, cols, cache->d, EVA_BF16, true, q_chunks(cache) + (T + 31) / 32).ws_bytes;
+}
+
+int eva_qtree_attention(const eva_qcache* cache, const void* q, const void* k, const void* v, const int* parents,
+                        const int* n_nodes, void* o, int T, const int* active, void* ws, size_t ws_bytes, void* stream) {
+    int st = check_qcache(cache);
+    if (st != EVA_OK) return st;
+    eva::TreeParams p{};
+    p.qc = qview_of(cache);
+    st = tree_nodes(p, k, v, parents, n_nodes, T, cache->W, cache->window);
+    if (st != EVA_OK) return st;
+    TreeRoute r;
+    st = tree_params(p, r, qgeometry_of(cache), cache->d, EVA_BF16, cache->n_tok, cache->max_tok, active, q, o, T, true,
+                     q_chunks(cache) + (T + 31) / 32, ws, ws_bytes);
+    if (st != EVA_OK) return st;
+    return launch_q(p, cache->d, stream);
+}
+
 }  // extern "C"

@@ -4,6 +4,7 @@
 
 #include <hip/hip_runtime.h>
 #include <stddef.h>
+#include <stdint.h>
 
 namespace eva {
 
@@ -287,5 +288,82 @@ inline int norm_rope_bwd_wgs(int tokens) {
 }
 template <int D, typename T>
 hipError_t launch_norm_rope_backward(const NormRopeParams& p, hipStream_t stream);
+
+// The 8-bit cache (qrows.hpp): codes and exponent bytes, per (b, kv head).
+struct QCacheView {
+    int B, H, Hkv, W, C, R, S_max;
+    int window;         // causal window variant
+    uint8_t* k_ring;    // [R][d]
+    uint8_t* vt_ring;   // [R / 16][d][16]
+    uint8_t* k_sum;     // [S_max][d]
+    uint8_t* vt_sum;    // [S_max / 16][d][16]
+    uint8_t* k_ring_e;  // [R]
+    uint8_t* v_ring_e;
+    uint8_t* k_sum_e;   // [S_max]
+    uint8_t* v_sum_e;
+};
+template <int D>
+hipError_t launch_qcache_fill(const QCacheView& c, const void* K, const void* V, const void* Ks, const void* Vs, int L,
+                              const int* lens, const RaggedState& r, hipStream_t stream);
+// Copies the rows of `c` (token counts n_tok, at most max_tok) into the bf16
+// cache `to` and sets its counts.
+template <int D>
+hipError_t launch_qcache_read(const QCacheView& c, const CacheView& to, const int* n_tok, int max_tok,
+                              const RaggedState& r, hipStream_t stream);
+
+// Tokens appended to a ragged cache: k, v [B][Hkv][T][d], of which sequence b
+// takes path[b][0 .. counts[b]).
+constexpr int kMaxPath = 64;
+struct PathParams {
+    const void* k;
+    const void* v;
+    const int* path;    // [B][T] or nullptr: 0, 1, ...
+    const int* counts;  // [B] or nullptr: T
+    int T;
+    int* n_tok;
+    int* arrive;
+    const int* active;
+    int max_tok;
+};
+template <int D, typename T>
+hipError_t launch_append_path(const CacheView& c, const PathParams& a, hipStream_t stream);
+template <int D>
+hipError_t launch_qappend_path(const QCacheView& c, const PathParams& a, hipStream_t stream);
+
+// Attention of drafted trees over a ragged cache, and of single queries over an
+// 8-bit one (tree.hip).
+struct TreeParams {
+    CacheView c;            // bf16 or fp32 cache; of an 8-bit one the geometry alone
+    QCacheView qc;
+    const int* n_tok;
+    const int* active;
+    int max_tok;
+    const void* q;          // [B][H][T][d]
+    void* o;
+    const void* k;          // [B][Hkv][T][d], nullptr: one query a sequence, of its last position
+    const void* v;
+    const int* parents;     // [B][T]
+    const int* n_nodes;     // [B] or nullptr: T
+    int T, G, cols;         // cols = G T query columns of a kv head
+    FastDiv fT;
+    int col_blocks, units;  // units = B Hkv
+    FastDiv f8cb, fHkv;     // divisors of 8 col_blocks and of Hkv
+    int splits;             // workgroups that share a row's keys
+    float* ws;              // their partials
+    float scale_log2, log2C;
+    int shape;              // TreeShape
+};
+// Workgroups: query columns of a kv head x waves that share their keys.
+enum TreeShape { kTreeNarrow, kTreeNarrowWide, kTree32, kTree64, kTree128 };
+constexpr int tree_shape_cols(int shape) { return shape <= kTreeNarrowWide ? 16 : shape == kTree32 ? 32 : shape == kTree64 ? 64 : 128; }
+constexpr int tree_shape_key_waves(int shape) {
+    return shape == kTreeNarrowWide ? 12 : shape == kTree128 ? 1 : shape == kTree64 ? 2 : 4;
+}
+// Q8: codes in p.qc; else bf16 rows in p.c.
+template <int D, bool Q8>
+hipError_t launch_tree(const TreeParams& p, hipStream_t stream);
+// Shapes of 16 columns only.
+template <int D>
+hipError_t launch_tree_f32(const TreeParams& p, hipStream_t stream);
 
 }  // namespace eva

@@ -1,0 +1,116 @@
+// Rows of the 8-bit cache (eva_qcache): d e4m3 codes and one exponent byte,
+// value = code 2^(byte - 127).  The exponent is the smallest whose power of
+// two brings the row's largest finite magnitude to 448, e4m3's largest value,
+// or below.  A power of two scales exactly both ways, so a code differs from
+// the row's value by its one rounding, the row's largest sum of squares has no
+// influence on it, and rows of the same values have the same codes wherever
+// they are quantised; a row's small entries lose nothing either, since the
+// codes have exponents of their own (2^-6 and less of 448 becomes subnormal).
+#pragma once
+
+#include "eva_device.hpp"
+#include "eva_kernels.hpp"
+
+namespace eva {
+
+// 16 slots of one feature are 16 contiguous bytes: row r, feature f of a
+// transposed value array lies at byte (r / 16) 16 D + 16 f + r % 16.
+constexpr int kQTile = 16;
+template <int D>
+__host__ __device__ __forceinline__ size_t qt_index(int f, int r) {
+    return (size_t)(r >> 4) * (kQTile * D) + (size_t)f * kQTile + (r & 15);
+}
+
+__device__ __forceinline__ bool is_finite(float x) { return fabsf(x) < INFINITY; }
+
+// Exponent byte of a row whose largest finite magnitude is amax.
+__device__ __forceinline__ uint32_t q_exponent(float amax) {
+    if (amax == 0.f) return 127;
+    // amax = m 2^e, 1/2 <= m < 1: 448 = 7/8 2^9
+    const int e = __builtin_amdgcn_frexp_expf(amax) - 9 + (__builtin_amdgcn_frexp_mantf(amax) > 0.875f ? 1 : 0);
+    return (uint32_t)(min(max(e, -126), 119) + 127);
+}
+__device__ __forceinline__ float q_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
+
+// Codes of eight features; inv = 2^-(byte - 127).  Values that are not finite
+// become e4m3's NaN.
+__device__ __forceinline__ u32x2 q_codes(const float x[8], float inv) {
+    float y[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = is_finite(x[i]) ? x[i] * inv : __uint_as_float(0x7fc00000u);
+    u32x2 w;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        int v = 0;
+        v = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * h], y[4 * h + 1], v, false);
+        v = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * h + 2], y[4 * h + 3], v, true);
+        w[h] = (uint32_t)v;
+    }
+    return w;
+}
+__device__ __forceinline__ float q_inverse(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
+
+// One row held by D / 8 neighbouring lanes of eight features: its exponent
+// byte (in every lane) and this lane's codes.
+template <int D>
+__device__ __forceinline__ uint32_t q_row(const float x[8], u32x2& codes) {
+    float amax = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) amax = fmaxf(amax, is_finite(x[i]) ? fabsf(x[i]) : 0.f);
+#pragma unroll
+    for (int off = 1; off < D / 8; off <<= 1) amax = fmaxf(amax, __shfl_xor(amax, off, 64));
+    const uint32_t byte = q_exponent(amax);
+    codes = q_codes(x, q_inverse(byte));
+    return byte;
+}
+
+// Value of one code.
+__device__ __forceinline__ float q_value(uint32_t code, float scale) {
+    return __builtin_amdgcn_cvt_f32_fp8((int)code, 0) * scale;
+}
+// Two codes (the low or high half of w) as bf16, exactly.
+template <bool HI>
+__device__ __forceinline__ uint32_t q_bf16x2(uint32_t w) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, HI));
+}
+// Eight codes as a matrix-core operand fragment.
+__device__ __forceinline__ bf16x8 q_bf16x8(uint32_t lo, uint32_t hi) {
+    return __builtin_bit_cast(bf16x8, u32x4{q_bf16x2<false>(lo), q_bf16x2<true>(lo), q_bf16x2<false>(hi), q_bf16x2<true>(hi)});
+}
+
+// Eight features of a row of T as fp32.
+__device__ __forceinline__ void row8(const bf16* p, float out[8]) {
+    const u32x4 w = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        out[2 * i] = bf16_lo(w[i]);
+        out[2 * i + 1] = bf16_hi(w[i]);
+    }
+}
+
+// Rows of a chunk in the 8-bit ring (the source of chunk_summary).
+template <int D>
+struct QRingChunk {
+    const uint8_t* k;   // this (b, g): [R][D]
+    const uint8_t* vt;  // [R / 16][D][16]
+    const uint8_t* ke;  // [R]
+    const uint8_t* ve;
+    long long pos0;
+    int R;
+    __device__ int slot(int r) const { return (int)((pos0 + r) % R); }
+    __device__ void load_k(int r, int cc, float out[8]) const {
+        const int s = slot(r);
+        const u32x2 w = *reinterpret_cast<const u32x2*>(k + (size_t)s * D + cc * 8);
+        const float sc = q_scale(ke[s]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) out[i] = q_value(w[i >> 2] >> (8 * (i & 3)), sc);
+    }
+    __device__ void load_v(int r, int cc, float out[8]) const {
+        const int s = slot(r);
+        const float sc = q_scale(ve[s]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) out[i] = q_value(vt[qt_index<D>(cc * 8 + i, s)], sc);
+    }
+};
+
+}  // namespace eva

@@ -546,3 +546,168 @@ def qk_norm_rope_backward(x, dQ, dK, dV, turns=None, q_weight=None, k_weight=Non
     _call(x.device, "eva_qk_norm_rope_backward", *args, *grads, _ptr(dx), _ptr(dg[0]), _ptr(dg[1]), _ptr(ws),
           ws.numel() * 4 if ws is not None else 0, B, H, Hkv, L, d, _dtype_code(x))
     return (dx, *dg)
+
+
+# ---- 8-bit cache -------------------------------------------------------------
+class QuantCache:
+    """Ragged decode cache of e4m3 rows with a power of two each (see
+    eva_qcache in eva.h): k_ring [B, Hkv, R, d], vt_ring [B, Hkv, R // 16, d, 16],
+    k_sum, vt_sum likewise over S_max, and each row's exponent byte in *_exp.
+    Queries, keys, values and outputs are bf16.  `max_tokens` bounds every
+    sequence."""
+
+    dtype = torch.bfloat16  # of the rows outside
+
+    def __init__(self, B, H, Hkv, d, W, C, max_tokens, device="cuda", R=None, fill=None,
+                 window=_lib.EVA_WINDOW_SLIDING):
+        if R is None:
+            R = -(-(W + C - 1) // 64) * 64
+        S_max = max(64, -(-(max_tokens // C + 1) // 64) * 64)
+        code = None if fill is None else int(torch.tensor(float(fill)).to(torch.float8_e4m3fn).view(torch.uint8))
+
+        def mk(*s, value=code):
+            t = torch.empty(*s, dtype=torch.uint8, device=device)
+            return t if code is None else t.fill_(value)
+
+        self.k_ring = mk(B, Hkv, R, d).view(torch.float8_e4m3fn)
+        self.vt_ring = mk(B, Hkv, R // 16, d, 16).view(torch.float8_e4m3fn)
+        self.k_sum = mk(B, Hkv, S_max, d).view(torch.float8_e4m3fn)
+        self.vt_sum = mk(B, Hkv, S_max // 16, d, 16).view(torch.float8_e4m3fn)
+        self.k_ring_exp, self.v_ring_exp = mk(B, Hkv, R, value=127), mk(B, Hkv, R, value=127)
+        self.k_sum_exp, self.v_sum_exp = mk(B, Hkv, S_max, value=127), mk(B, Hkv, S_max, value=127)
+        self.n_tok = torch.zeros(B, dtype=torch.int32, device=device)
+        self.arrive = torch.zeros(B, dtype=torch.int32, device=device)
+        names = ("n_tok", "arrive", "k_ring", "vt_ring", "k_sum", "vt_sum", "k_ring_exp", "v_ring_exp", "k_sum_exp",
+                 "v_sum_exp")
+        self.struct = _lib.EvaQCacheStruct(B=B, H=H, H_kv=Hkv, d=d, W=W, C=C, window=window, R=R, S_max=S_max,
+                                           max_tok=max_tokens, **{n: getattr(self, n).data_ptr() for n in names})
+
+    @property
+    def R(self) -> int:
+        return int(self.struct.R)
+
+    @property
+    def S_max(self) -> int:
+        return int(self.struct.S_max)
+
+
+def _of_cache(cache, t, what, shape):
+    """An operand in the cache's dtype, contiguous and on its device."""
+    return _expect(t, what, shape, cache.dtype, cache.n_tok.device)
+
+
+def _ints(cache, t, what, shape):
+    return _expect(t, what, shape, torch.int32, cache.n_tok.device)
+
+
+def _scratch(cache, n):
+    """(pointer, bytes, tensor) of a workspace of n bytes."""
+    if n == 0:
+        return None, 0, None
+    ws = torch.empty((n + 3) // 4, dtype=torch.float32, device=cache.n_tok.device)
+    return ws.data_ptr(), n, ws
+
+
+def _rows_out(cache, q, out, whole):
+    """The output of q's shape: `out`, or a new one (zeros where the call may
+    leave rows unwritten)."""
+    if out is None:
+        return torch.empty_like(q) if whole else torch.zeros_like(q)
+    _of_cache(cache, out, "out", q.shape)
+    return out
+
+
+def qcache_fill(cache: QuantCache, K, V, Ks, Vs, lens):
+    """rcache_fill into an 8-bit cache: K, V [B, Hkv, L, d] and their summaries,
+    quantised; lens (int32 [B]) are the valid lengths."""
+    s = cache.struct
+    B, Hkv, L, d = K.shape
+    shape, sums = (s.B, s.H_kv, L, s.d), (s.B, s.H_kv, L // s.C, s.d)
+    _call(cache.n_tok.device, "eva_qcache_fill", ctypes.byref(s), _of_cache(cache, K, "K", shape),
+          _of_cache(cache, V, "V", shape), _of_cache(cache, Ks, "Ks", sums), _of_cache(cache, Vs, "Vs", sums), L,
+          _ints(cache, lens, "lens", (s.B,)))
+
+
+def qcache_append(cache: QuantCache, k_new, v_new, active=None):
+    """Append one token to each active sequence: k_new, v_new [B, Hkv, d]."""
+    s = cache.struct
+    row = (s.B, s.H_kv, s.d)
+    _call(cache.n_tok.device, "eva_qcache_append", ctypes.byref(s), _of_cache(cache, k_new, "k_new", row),
+          _of_cache(cache, v_new, "v_new", row), _ints(cache, active, "active", (s.B,)))
+
+
+def qcache_read(cache: QuantCache, to: RaggedCache) -> RaggedCache:
+    """Copy the 8-bit cache's rows and token counts into the bf16 ragged cache
+    `to` of the same geometry, which can then go on with them."""
+    if to.n_tok.device != cache.n_tok.device:
+        raise RuntimeError("both caches must be on one device")
+    _call(cache.n_tok.device, "eva_qcache_read", ctypes.byref(cache.struct), ctypes.byref(to.struct))
+    return to
+
+
+def qdecode_step(cache: QuantCache, q, active=None, out=None, use_workspace=True):
+    """rdecode_step over an 8-bit cache: q [B, H, d] -> o [B, H, d].  Rows of
+    inactive or empty sequences keep the contents of `out`."""
+    s = cache.struct
+    qp = _of_cache(cache, q, "q", (s.B, s.H, s.d))
+    o = _rows_out(cache, q, out, False)
+    n = _lib.load().eva_qdecode_workspace_bytes(ctypes.byref(s)) if use_workspace else 0
+    wp, nbytes, ws = _scratch(cache, n)
+    _call(cache.n_tok.device, "eva_qdecode_step", ctypes.byref(s), qp, _ptr(o), _ints(cache, active, "active", (s.B,)),
+          wp, nbytes)
+    return o
+
+
+def qappend_decode(cache: QuantCache, q, k_new, v_new, active=None, out=None, use_workspace=True):
+    """qcache_append(k_new, v_new), then qdecode_step(q)."""
+    s = cache.struct
+    row = (s.B, s.H_kv, s.d)
+    args = (_of_cache(cache, q, "q", (s.B, s.H, s.d)), _of_cache(cache, k_new, "k_new", row),
+            _of_cache(cache, v_new, "v_new", row))
+    o = _rows_out(cache, q, out, False)
+    n = _lib.load().eva_qdecode_workspace_bytes(ctypes.byref(s)) if use_workspace else 0
+    wp, nbytes, ws = _scratch(cache, n)
+    _call(cache.n_tok.device, "eva_qappend_decode", ctypes.byref(s), *args, _ptr(o),
+          _ints(cache, active, "active", (s.B,)), wp, nbytes)
+    return o
+
+
+# ---- drafted trees -----------------------------------------------------------
+def tree_attention(cache, q, k, v, parents, n_nodes=None, active=None, out=None, use_workspace=True):
+    """Rows of a tree of drafted tokens for every sequence of a RaggedCache or
+    QuantCache, which is left as it is: q [B, H, T, d], k, v [B, Hkv, T, d] ->
+    o [B, H, T, d].
+
+    parents (int32 [B, T]): the earlier node that node t continues, or -1: the
+    sequence itself.  n_nodes (int32 [B]): each tree's size, T if None.  Node t's
+    position is n_tok[b] + its depth.  T is at most 64 and W.  Rows of inactive
+    sequences and absent nodes keep the contents of `out`."""
+    s = cache.struct
+    if q.dim() != 4:
+        raise ValueError("q must be [B, H, T, d]")
+    T = q.shape[2]
+    row = (s.B, s.H_kv, T, s.d)
+    args = (_of_cache(cache, q, "q", (s.B, s.H, T, s.d)), _of_cache(cache, k, "k", row), _of_cache(cache, v, "v", row),
+            _ints(cache, parents, "parents", (s.B, T)), _ints(cache, n_nodes, "n_nodes", (s.B,)))
+    o = _rows_out(cache, q, out, n_nodes is None and active is None)
+    kind = "eva_q" if isinstance(cache, QuantCache) else "eva_r"
+    n = getattr(_lib.load(), kind + "tree_workspace_bytes")(ctypes.byref(s), T) if use_workspace else 0
+    wp, nbytes, ws = _scratch(cache, n)
+    _call(cache.n_tok.device, kind + "tree_attention", ctypes.byref(s), *args, _ptr(o), T,
+          _ints(cache, active, "active", (s.B,)), wp, nbytes)
+    return o
+
+
+def append_path(cache, k, v, path=None, counts=None, active=None):
+    """Append an accepted path to every active sequence of a RaggedCache or
+    QuantCache: the tokens path[b, :counts[b]] (int32 [B, T], [B]; by default
+    all T in their order) of k, v [B, Hkv, T, d]."""
+    s = cache.struct
+    if k.dim() != 4:
+        raise ValueError("k must be [B, Hkv, T, d]")
+    T = k.shape[2]
+    row = (s.B, s.H_kv, T, s.d)
+    _call(cache.n_tok.device, ("eva_q" if isinstance(cache, QuantCache) else "eva_r") + "append_path",
+          ctypes.byref(s), _of_cache(cache, k, "k", row), _of_cache(cache, v, "v", row),
+          _ints(cache, path, "path", (s.B, T)), _ints(cache, counts, "counts", (s.B,)), T,
+          _ints(cache, active, "active", (s.B,)))
