@@ -992,18 +992,16 @@ struct TreeRoute {
 };
 TreeRoute tree_route(long long units, long long cols, int d, int dtype, bool drafted, int n_chunks) {
     TreeRoute r;
-    r.shape = eva::kTreeNarrow;
-    if (dtype == EVA_BF16 && drafted)
-        r.shape = cols <= 16 ? eva::kTreeNarrow : cols <= 32 ? eva::kTree32 : cols <= 64 ? eva::kTree64 : eva::kTree128;
-    const int per = eva::tree_shape_cols(r.shape);
+    const bool wide = dtype == EVA_BF16 && drafted && cols > 32;
+    r.shape = !wide ? eva::kTreeNarrow : cols <= 64 ? eva::kTree64 : eva::kTree128;
+    const int per = !wide ? 16 : cols <= 64 ? 64 : 128;
     const long long blocks = (cols + per - 1) / per, wgs = units * blocks;
     r.col_blocks = (int)blocks;
-    if (r.shape == eva::kTreeNarrow && wgs < 256 && n_chunks > 4 && n_chunks <= 20) r.shape = eva::kTreeNarrowWide;
-    const int kw = eva::tree_shape_key_waves(r.shape);
+    if (!wide && wgs < 256 && n_chunks > 4 && n_chunks <= 20) r.shape = eva::kTreeNarrow12;
     r.splits = 1;
-    if (r.shape != eva::kTreeNarrowWide && wgs < 256) {
+    if (r.shape != eva::kTreeNarrow12 && wgs < 256) {
         long long s = (512 + wgs - 1) / wgs;
-        const long long most = (n_chunks + kw - 1) / kw;
+        const long long most = (n_chunks + 3) / 4;
         r.splits = (int)(s > most ? most : s);
     }
     r.ws_bytes = r.splits > 1 ? (size_t)units * r.splits * cols * (d + 2) * sizeof(float) : 0;

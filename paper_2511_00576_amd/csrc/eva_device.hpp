@@ -142,6 +142,14 @@ __device__ __forceinline__ T* uniform_ptr(T* p) {
     return reinterpret_cast<T*>((uint64_t)hi << 32 | lo);
 }
 
+// The lane id, computed where it is used: a value that depends on the lane
+// kept over the block loop only for the rare masks would take a register.
+__device__ __forceinline__ int lane_here() {
+    int l;
+    asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=&v"(l));
+    return l;
+}
+
 // Counter-based normal draws for the stochastic summaries, so that the draw
 // of chunk c of sequence-head s is the same wherever its summary is built.
 // Philox4x32-10 (Salmon, Moraes, Dror, Shaw, SC 2011): ten rounds over a

@@ -353,15 +353,14 @@ struct TreeParams {
     float scale_log2, log2C;
     int shape;              // TreeShape
 };
-// Workgroups: query columns of a kv head x waves that share their keys.
-enum TreeShape { kTreeNarrow, kTreeNarrowWide, kTree32, kTree64, kTree128 };
-constexpr int tree_shape_cols(int shape) { return shape <= kTreeNarrowWide ? 16 : shape == kTree32 ? 32 : shape == kTree64 ? 64 : 128; }
-constexpr int tree_shape_key_waves(int shape) {
-    return shape == kTreeNarrowWide ? 12 : shape == kTree128 ? 1 : shape == kTree64 ? 2 : 4;
-}
+// Workgroups of 16 columns and 4 or 12 waves that share their keys (tree.hip), or of
+// 64 or 128 columns (tree_wide.hip).
+enum TreeShape { kTreeNarrow, kTreeNarrow12, kTree64, kTree128 };
 // Q8: codes in p.qc; else bf16 rows in p.c.
 template <int D, bool Q8>
 hipError_t launch_tree(const TreeParams& p, hipStream_t stream);
+template <int D, bool Q8>
+hipError_t launch_tree_wide(const TreeParams& p, hipStream_t stream);
 // Shapes of 16 columns only.
 template <int D>
 hipError_t launch_tree_f32(const TreeParams& p, hipStream_t stream);

@@ -155,14 +155,6 @@ __device__ __forceinline__ float row_lanes_sum(float x) {
     return x;
 }
 
-// The lane id, computed where it is used: a value that depends on the lane
-// kept over the block loop only for the rare masks would take a register.
-__device__ __forceinline__ int lane_here() {
-    int l;
-    asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=&v"(l));
-    return l;
-}
-
 // Elements of a score tile whose block row x (less h2 KH) is above hi / below lo to -inf.
 template <int D>
 __device__ __forceinline__ void mask_above(floatx16& s, int hi) {
