@@ -12,10 +12,10 @@ constexpr int kMaxNodes = 64;
 // Lines of the tree's nodes: lane t holds the set of node t's forerunners and
 // itself.  Parents name an earlier node; any other value makes a root.  Six
 // rounds of doubling reach 64 nodes back.
-__device__ __forceinline__ unsigned long long tree_lines(const int* parents, int nodes) {
+// parent: lane t's entry of the parents.
+__device__ __forceinline__ unsigned long long tree_lines(int parent, int nodes) {
     const int lane = threadIdx.x & 63;
-    int up = lane < nodes ? parents[lane] : -1;
-    if (up < 0 || up >= lane) up = -1;
+    int up = lane < nodes && parent >= 0 && parent < lane ? parent : -1;
     unsigned long long line = 1ull << lane;
 #pragma unroll
     for (int r = 0; r < 6; ++r) {
@@ -40,6 +40,9 @@ struct TreeRows {
     int lo_first, lo_last, sum_first, sum_last;
     bool any;                  // there is a row to compute
     __device__ __forceinline__ TreeRows(const TreeParams& a, int b, bool drafted) {
+        // (all of the sequence's words requested at once)
+        const int lane = threadIdx.x & 63;
+        const int parent = drafted ? a.parents[(size_t)b * a.T + min(lane, a.T - 1)] : 0;
         n = min(max(a.n_tok[b], 0), a.max_tok);
         nodes = !drafted ? 1 : a.n_nodes ? min(max(a.n_nodes[b], 0), a.T) : a.T;
         any = !(a.active && a.active[b] == 0) && (drafted ? nodes : n) > 0;
@@ -49,8 +52,7 @@ struct TreeRows {
         if (!any) return;
         int deepest = 0;
         if (drafted) {
-            lines = tree_lines(a.parents + (size_t)b * a.T, nodes);
-            const int lane = threadIdx.x & 63;
+            lines = tree_lines(parent, nodes);
             deepest = lane < nodes ? __builtin_popcountll(lines) - 1 : 0;
 #pragma unroll
             for (int off = 1; off < 64; off <<= 1) deepest = max(deepest, __shfl_xor(deepest, off, 64));

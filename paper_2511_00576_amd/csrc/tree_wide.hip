@@ -3,12 +3,12 @@
 // so that they are fetched once for 32 WC columns.  The decode's direct reads
 // (tree.hip) would fetch them from the L1 for every 16.
 //
-// Blocks: 32 rows of a bf16 cache or 64 of an 8-bit one (the same bytes),
-// summaries first, then the window, then the drafted tokens (32 rows, bf16).
-// They are requested by LDS DMA two ahead into a ring of three stages.  A wave
+// Blocks: summaries first, then the window, then the drafted tokens (32 rows,
+// bf16).  They are requested ahead by LDS DMA into a ring of stages.  A wave
 // holds 32 columns; S^T = K Q^T, then O^T += V^T P^T on 32x32x16 products.  With
-// WC = 4 column waves every wave takes every block, with WC = 2 the two key
-// waves of a column wave take turns and are joined at the end.
+// WC = 4 column waves every wave takes a whole block (32 rows, or 64 of an 8-bit
+// cache: the same bytes); with WC = 2 blocks are 64 rows, the two key waves of
+// a column wave take 32 each and are joined at the end.
 //
 // The cache's values lie transposed, 8 (16) keys of a feature in 16 bytes: their
 // fragments are plain 16-byte reads, and the rows of S^T are permuted so that a
@@ -27,15 +27,15 @@ namespace {
 // A block of the cache in LDS: rows in groups of 1 KB, one DMA instruction each.
 // The skew between groups and the swizzle of a row's 16-byte chunks spread the
 // 16 rows of a fragment read over the banks.
-template <int D, bool Q8>
+template <int D, bool Q8, int WC>
 struct CacheTile {
-    static constexpr int KEYS = Q8 ? 64 : 32;
+    static constexpr int KEYS = Q8 || WC == 2 ? 64 : 32;
     static constexpr int ROWB = Q8 ? D : 2 * D;
     static constexpr int RPI = 1024 / ROWB;
     static constexpr int GRP = 1024 + (Q8 ? 32 : 64);
     static constexpr int GROUPS = KEYS * ROWB / 1024;
     static constexpr int NI = GROUPS / 4;  // requests per wave
-    static constexpr int SUB = KEYS / 32;  // score tiles
+    static constexpr int SUB = KEYS / 32 / (4 / WC);  // 32-key sub-blocks of a wave
     static __device__ __forceinline__ int row_at(int r) { return r / RPI * GRP + r % RPI * ROWB; }
     static __device__ __forceinline__ int swz(int r) { return (ROWB == 256 ? r : ROWB == 128 ? r >> 1 : r >> 2) & 3; }
     // key, within a 32-key sub-block, of product row m = 8 q + 4 h + i
@@ -47,12 +47,13 @@ struct CacheTile {
     static __device__ __forceinline__ int key_of(int i, int h) { return Q8 ? 16 * h + i : 16 * (i >> 3) + 8 * h + (i & 7); }
 };
 
-template <int D, bool Q8>
+template <int D, bool Q8, int WC>
 struct WideStage {
-    static constexpr int BLK = CacheTile<D, Q8>::GROUPS * CacheTile<D, Q8>::GRP > Tile<D>::BLK
-                                   ? CacheTile<D, Q8>::GROUPS * CacheTile<D, Q8>::GRP : Tile<D>::BLK;
+    typedef CacheTile<D, Q8, WC> T;
+    static constexpr int BLK = T::GROUPS * T::GRP > Tile<D>::BLK ? T::GROUPS * T::GRP : Tile<D>::BLK;
     static constexpr int EXP = Q8 ? 4 * 512 : 0;  // exponent bytes, a copy per wave: 64 of the keys, 64 of the values
     static constexpr int BYTES = 2 * BLK + EXP;
+    static constexpr int NS = BYTES > 24 * 1024 ? 2 : 3;  // stages: two workgroups a CU at least
 };
 
 // Two of a raw 16-byte read's contraction steps: the low or high eight codes.
@@ -75,13 +76,13 @@ __device__ __forceinline__ void stream_reads(Load&& load, Use&& use) {
 
 template <int D, bool Q8, int WC>
 __global__ __launch_bounds__(256, 2) void tree_wide_kernel(TreeParams a) {
-    typedef CacheTile<D, Q8> T;
+    typedef CacheTile<D, Q8, WC> T;
     typedef Tile<D> DT;
-    typedef WideStage<D, Q8> Stage;
-    constexpr int WK = 4 / WC, SUB = T::SUB;
+    typedef WideStage<D, Q8, WC> Stage;
+    constexpr int WK = 4 / WC, SUB = T::SUB, NS = Stage::NS;
     constexpr int NDC = D / 16, NDB = D / 32;
     constexpr int NIT = 2 * T::NI + (Q8 ? 2 : 0);  // requests per wave and block
-    static_assert(DT::NI == T::NI, "drafted blocks take as many requests");
+    static_assert(DT::NI <= T::NI, "drafted blocks take no more requests");
     extern __shared__ __attribute__((aligned(1024))) unsigned char wide_smem[];
 
     const TreePlace place(a);
@@ -158,8 +159,14 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(TreeParams a) {
             const u32x4 dk = rows_desc<D>((uintptr_t)a.k + at, there), dv = rows_desc<D>((uintptr_t)a.v + at, there);
             dma_block<D>(dk, dk_off, base + wave * DT::GRP);
             dma_block<D>(dv, dv_off, base + Stage::BLK + wave * DT::GRP);
-            if constexpr (Q8) {  // as many requests as any block has
-                const u32x4 none{0, 0, 0, 0x00020000u};
+            // as many requests as any block has: zeros to places of no use now
+            const u32x4 none{0, 0, 0, 0x00020000u};
+#pragma unroll
+            for (int i = DT::NI; i < T::NI; ++i) {
+                dma16(none, v_off, 0, base + (4 * i + wave) * T::GRP);
+                dma16(none, v_off, 0, base + Stage::BLK + (4 * i + wave) * T::GRP);
+            }
+            if constexpr (Q8) {
                 const unsigned to = base + 2 * Stage::BLK + wave * 512;
                 dma4(none, lane * 4, to);
                 dma4(none, lane * 4, to + 256);
@@ -167,8 +174,8 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(TreeParams a) {
         }
     };
     if (j0 < j1) {
-        request(j0, 0);
-        request(j0 + 1, 1);
+#pragma unroll
+        for (int i = 0; i < NS - 1; ++i) request(j0 + i, i);
     }
 
     // ---- the wave's columns ----
@@ -229,6 +236,7 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(TreeParams a) {
             full = pos0 >= rows.lo_last && key_hi == T::KEYS - 1;
         }
         const float bias = is_sum ? a.log2C : 0.f;
+        const int sub0 = WK == 2 ? wk : 0;  // the wave's first sub-block
         floatx16 s[SUB];
         u32x4 vx[SUB];
 #pragma unroll
@@ -237,7 +245,7 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(TreeParams a) {
         stream_reads<SUB * KR>(
             [&](int k) {
                 const int p = k % KR;
-                return *reinterpret_cast<const u32x4*>(ks + k / KR * (32 / T::RPI * T::GRP) + ((p & 1) ? kr1 : kr0) + (p >> 1) * 64);
+                return *reinterpret_cast<const u32x4*>(ks + (sub0 + k / KR) * (32 / T::RPI * T::GRP) + ((p & 1) ? kr1 : kr0) + (p >> 1) * 64);
             },
             [&](int k, const u32x4& w) {
                 floatx16& o = s[k / KR];
@@ -252,7 +260,7 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(TreeParams a) {
         if constexpr (Q8) {
 #pragma unroll
             for (int sb = 0; sb < SUB; ++sb) {
-                const unsigned char* ex = st + 2 * Stage::BLK + wave * 512 + 32 * sb + 16 * h2;
+                const unsigned char* ex = st + 2 * Stage::BLK + wave * 512 + 32 * (sub0 + sb) + 16 * h2;
                 const u32x4 kx = *reinterpret_cast<const u32x4*>(ex);
                 vx[sb] = *reinterpret_cast<const u32x4*>(ex + 256);
 #pragma unroll
@@ -260,7 +268,7 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(TreeParams a) {
             }
         }
         if (!full) {
-            const int half = T::key_of(0, lane_here() >> 5);
+            const int half = T::key_of(0, lane_here() >> 5) + 32 * sub0;
             const int first = (is_sum ? 0 : max(lo - pos0, key_lo)) - half;
             const int last = (is_sum ? min(n_sum - pos0 - 1, key_hi) : key_hi) - half;
 #pragma unroll
@@ -293,15 +301,16 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(TreeParams a) {
                 }
                 pf[sb][i >> 3][(i & 7) >> 1] = pack_bf16x2(p0, p1);
             }
-        // values: tile (16 bytes a feature) 2 x + h2, x = kc (8-bit: sub-block)
-        constexpr int TILEB = D * 16;
+        // values: 16 bytes a feature are 8 keys, tile 4 sub + 2 kc + h2, or 16
+        // codes, tile 2 sub + h2
+        constexpr int TILEB = D * 16, VR = Q8 ? SUB : 2;  // tiles read by a lane
         auto vfrag = [&](int x, int db) {
-            const int byte = (2 * x + h2) * TILEB + (32 * db + c32) * 16;
+            const int byte = ((Q8 ? 2 * (sub0 + x) : 4 * sub0 + 2 * x) + h2) * TILEB + (32 * db + c32) * 16;
             return *reinterpret_cast<const u32x4*>(vs + (byte >> 10) * T::GRP + (byte & 1023));
         };
         // Of a block with an edge a column may not see what others see, and slots
         // may be stale: whatever bits they hold, their weights are 0
-        stream_reads<2 * NDB>([&](int k) { return vfrag(k / NDB, k % NDB); },
+        stream_reads<VR * NDB>([&](int k) { return vfrag(k / NDB, k % NDB); },
                               [&](int k, const u32x4& w) {
                                   const int x = k / NDB;
                                   if constexpr (Q8) {
@@ -313,6 +322,7 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(TreeParams a) {
                               });
     };
     auto draft_block = [&](int j, const unsigned char* st) {
+        if (WK == 2 && ((j - cache_blocks) & 1) != wk) return;  // the key waves take turns
         const unsigned char *ks = st, *vs = st + Stage::BLK;
         const int k0 = (j - cache_blocks) * 32;
         floatx16 s = floatx16{};
@@ -352,16 +362,16 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(TreeParams a) {
     int stage = 0;
     auto steps = [&](int from, int to, auto&& block) {
         for (int j = from; j < to; ++j) {
-            // block j landed (the one after it may stay in flight); the block
+            // block j landed (of three stages the next may stay in flight); the block
             // requested now refills the stage whose last reads were before this barrier
             asm volatile("" ::: "memory");
-            wait_vm_lgkm0<NIT>();
+            wait_vm_lgkm0<(NS - 2) * NIT>();
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
-            request(j + 2, stage == 0 ? 2 : stage - 1);
+            request(j + NS - 1, stage == 0 ? NS - 1 : stage - 1);
             const unsigned char* st = wide_smem + stage * Stage::BYTES;
-            stage = stage == 2 ? 0 : stage + 1;
-            if (WK == 1 || (j & (WK - 1)) == wk) block(j, st);
+            stage = stage == NS - 1 ? 0 : stage + 1;
+            block(j, st);
         }
     };
     steps(j0, min(j1, cache_blocks), cache_block);
@@ -449,10 +459,11 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(TreeParams a) {
     }
 }
 
-template <int D, bool Q8>
-constexpr size_t wide_lds(int wk) {
-    const size_t ring = 3 * (size_t)WideStage<D, Q8>::BYTES;
-    const size_t end = wk == 2 ? 2 * 32 * (size_t)(D + 6) * 4 : 4 * 32 * (size_t)kStageRow<D>;
+template <int D, bool Q8, int WC>
+constexpr size_t wide_lds() {
+    typedef WideStage<D, Q8, WC> Stage;
+    const size_t ring = (size_t)Stage::NS * Stage::BYTES;
+    const size_t end = WC == 2 ? 2 * 32 * (size_t)(D + 6) * 4 : 4 * 32 * (size_t)kStageRow<D>;
     return ring > end ? ring : end;
 }
 
@@ -462,9 +473,9 @@ template <int D, bool Q8>
 hipError_t launch_tree_wide(const TreeParams& p, hipStream_t stream) {
     const dim3 grid((unsigned)((p.units + 7) / 8 * 8 * p.col_blocks), (unsigned)p.splits);
     if (p.shape == kTree64)
-        hipLaunchKernelGGL((tree_wide_kernel<D, Q8, 2>), grid, dim3(256), (wide_lds<D, Q8>(2)), stream, p);
+        hipLaunchKernelGGL((tree_wide_kernel<D, Q8, 2>), grid, dim3(256), (wide_lds<D, Q8, 2>()), stream, p);
     else
-        hipLaunchKernelGGL((tree_wide_kernel<D, Q8, 4>), grid, dim3(256), (wide_lds<D, Q8>(1)), stream, p);
+        hipLaunchKernelGGL((tree_wide_kernel<D, Q8, 4>), grid, dim3(256), (wide_lds<D, Q8, 4>()), stream, p);
     return hipGetLastError();
 }
 template hipError_t launch_tree_wide<64, false>(const TreeParams&, hipStream_t);
