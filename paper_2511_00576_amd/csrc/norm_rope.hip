@@ -43,6 +43,26 @@ __device__ __forceinline__ void load8(const float* p, float out[8]) {
         for (int i = 0; i < 4; ++i) out[4 * h + i] = w[i];
     }
 }
+// A lane's 16 features of a row as they lie in memory.
+template <typename T>
+struct RawRow {
+    static constexpr int N = (int)sizeof(T);  // 16-byte pieces
+    u32x4 w[N];
+    __device__ __forceinline__ void load(const T* row, int f0, int f1) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            w[i] = *reinterpret_cast<const u32x4*>(row + (i < N / 2 ? f0 : f1) + i % (N / 2) * (16 / sizeof(T)));
+    }
+    __device__ __forceinline__ void values(float (&x)[16]) const {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            if constexpr (sizeof(T) == 2)
+                x[i] = (i & 1) ? bf16_hi(w[i / 8][i % 8 / 2]) : bf16_lo(w[i / 8][i % 8 / 2]);
+            else
+                x[i] = __uint_as_float(w[i / 4][i % 4]);
+        }
+    }
+};
 __device__ __forceinline__ void store8(bf16* p, const float x[8]) {
     *reinterpret_cast<u32x4*>(p) = u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
                                          pack_bf16x2(x[6], x[7])};
@@ -101,20 +121,29 @@ struct LaneRow {
     }
 };
 
+// cos and sin of t 2^-64 turns.  The nearest quarter turn is taken off the whole
+// number, exactly; what is left, at most pi / 4, goes into the Taylor series to
+// x^9 and x^10, whose next terms are below 2^-29 and 2^-35.
+__device__ __forceinline__ void cos_sin(unsigned long long t, float& c, float& s) {
+    const uint32_t hi = (uint32_t)(t >> 32);
+    const uint32_t quarter = (hi + 0x20000000u) >> 30;
+    const float x = (float)(int)(hi - (quarter << 30)) * 1.4629180792671596e-9f;  // 2 pi 2^-32
+    const float z = x * x;
+    const float sn = fmaf(fmaf(fmaf(fmaf(2.7557319e-6f, z, -1.9841270e-4f), z, 8.3333333e-3f), z, -1.6666667e-1f) * z, x, x);
+    const float cs = fmaf(fmaf(fmaf(fmaf(fmaf(-2.7557319e-7f, z, 2.4801587e-5f), z, -1.3888889e-3f), z, 4.1666667e-2f), z, -0.5f), z, 1.f);
+    const float u = (quarter & 1) ? sn : cs, v = (quarter & 1) ? cs : sn;
+    c = ((quarter + 1) & 2) ? -u : u;
+    s = (quarter & 2) ? -v : v;
+}
+
 // cos and sin of the lane's eight pairs at a token's position.
 template <int D, bool ADJ>
-__device__ void angles(const NormRopeParams& a, const LaneRow<D, ADJ>& r, int tok, float (&cs)[8], float (&sn)[8]) {
+__device__ __forceinline__ void angles(const NormRopeParams& a, const LaneRow<D, ADJ>& r, int tok, float (&cs)[8], float (&sn)[8]) {
     if (!r.turned) return;
     const int b = tok / a.fL, l = tok - b * a.fL.d;
     const long long pos = (long long)(a.start ? a.start[b] : 0) + (a.offsets ? a.offsets[tok] : l);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const unsigned long long t = (unsigned long long)pos * a.turns[8 * r.c + j];
-        // half turns in [-1, 1)
-        const float x = (float)(int)(t >> 32) * 4.656612873077393e-10f;
-        cs[j] = cospif(x);
-        sn[j] = sinpif(x);
-    }
+    for (int j = 0; j < 8; ++j) cos_sin((unsigned long long)pos * a.turns[8 * r.c + j], cs[j], sn[j]);
 }
 
 // Sweeps of a token: kRows heads each, queries first, then keys, then values.
@@ -137,36 +166,45 @@ __global__ __launch_bounds__(kNormRopeWaves * 64) void norm_rope_kernel(NormRope
     const int b = tok / a.fL, l = tok - b * a.fL.d;
     const Sweeps sw(a, r.kRows);
     const T* xt = static_cast<const T*>(a.x) + b * a.stride_b + l * a.stride_l;
+    // sweep s: its heads are `heads` from the row's `first` on, this lane's is h
+    struct Sweep {
+        int kind, first, heads, h;  // kind 0 queries, 1 keys, 2 values
+    };
+    auto sweep = [&](int s) {
+        const int kind = s < sw.q ? 0 : s < sw.k ? 1 : 2;
+        return Sweep{kind, kind == 0 ? 0 : kind == 1 ? a.H : a.H + a.Hkv, kind == 0 ? a.H : a.Hkv,
+                     (s - (kind == 0 ? 0 : kind == 1 ? sw.q : sw.k)) * r.kRows + r.sub};
+    };
+    RawRow<T> raw;
+    auto request = [&](const Sweep& w) { raw.load(xt + (size_t)(w.first + min(w.h, w.heads - 1)) * D, r.f0, r.f1); };
+    // rows are requested a sweep ahead, the first before the angles
+    Sweep w = sweep(blockIdx.y);
+    request(w);
     float cs[8], sn[8];
     angles(a, r, tok, cs, sn);
     for (int s = blockIdx.y; s < sw.all; s += gridDim.y) {
-        if (s < sw.k) {
-            const bool key = s >= sw.q;
-            const int heads = key ? a.Hkv : a.H;
-            const int h = (key ? s - sw.q : s) * r.kRows + r.sub;
-            if (h >= heads) continue;
-            float y[16];
-            r.load(xt + (size_t)((key ? a.H : 0) + h) * D, y);
-            const T* g = static_cast<const T*>(key ? a.gk : a.gq);
+        float y[16];
+        raw.values(y);
+        const Sweep now = w;
+        if (s + (int)gridDim.y < sw.all) {
+            w = sweep(s + gridDim.y);
+            request(w);
+        }
+        T* out = static_cast<T*>(now.kind == 0 ? a.Q : now.kind == 1 ? a.K : a.V);
+        if (now.kind < 2) {
+            const T* g = static_cast<const T*>(now.kind ? a.gk : a.gq);
             if (g) {
-                float w[16], ss = 0.f;
-                r.load(g, w);
+                float wt[16], ss = 0.f;
+                r.load(g, wt);
 #pragma unroll
                 for (int i = 0; i < 16; ++i) ss += y[i] * y[i];
                 const float inv = rsqrtf(r.sum(ss) * (1.f / D) + a.eps);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) y[i] = y[i] * inv * w[i];
+                for (int i = 0; i < 16; ++i) y[i] = y[i] * inv * wt[i];
             }
             r.template turn<1>(y, cs, sn);
-            T* out = static_cast<T*>(key ? a.K : a.Q);
-            r.store(out + (((size_t)b * heads + h) * a.fL.d + l) * D, y);
-        } else {
-            const int h = (s - sw.k) * r.kRows + r.sub;
-            if (h >= a.Hkv) continue;
-            float y[16];
-            r.load(xt + (size_t)(a.H + a.Hkv + h) * D, y);
-            r.store(static_cast<T*>(a.V) + (((size_t)b * a.Hkv + h) * a.fL.d + l) * D, y);
         }
+        if (now.h < now.heads) r.store(out + (((size_t)b * now.heads + now.h) * a.fL.d + l) * D, y);
     }
 }
 
@@ -175,7 +213,7 @@ __global__ __launch_bounds__(kNormRopeWaves * 64) void norm_rope_kernel(NormRope
 // the workspace, and a second launch adds those up in their order: the same
 // bits every time.
 template <int D, typename T, bool ADJ>
-__global__ __launch_bounds__(kNormRopeWaves * 64) void norm_rope_bwd_kernel(NormRopeParams a) {
+__global__ __launch_bounds__(kNormRopeWaves * 64, 3) void norm_rope_bwd_kernel(NormRopeParams a) {
     const LaneRow<D, ADJ> r(a);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Sweeps sw(a, r.kRows);
@@ -244,22 +282,33 @@ __global__ __launch_bounds__(kNormRopeWaves * 64) void norm_rope_bwd_kernel(Norm
     }
 }
 
-// Sums the n workgroups' shares of 16 features: a row of 16 threads a share.
+// Sums the n workgroups' shares of 8 features: 128 threads a feature, each with
+// its loads of eight shares in flight together, then their sums in a fixed
+// order.  (16 threads a feature, one load after the other, took 20 us for 1024
+// shares.)
+constexpr int kSumFeatures = 8;
 template <int D>
-__global__ __launch_bounds__(256) void norm_rope_sum_kernel(const float* __restrict__ ws, int n, float* dgq, float* dgk) {
-    __shared__ float part[16][17];
-    const int f = threadIdx.x % 16, r = threadIdx.x / 16;
-    const int e = blockIdx.x * 16 + f;
+__global__ __launch_bounds__(1024) void norm_rope_sum_kernel(const float* __restrict__ ws, int n, float* dgq, float* dgk) {
+    constexpr int R = 1024 / kSumFeatures;
+    __shared__ float part[R][kSumFeatures + 1];
+    const int f = threadIdx.x % kSumFeatures, r = threadIdx.x / kSumFeatures;
+    const int e = blockIdx.x * kSumFeatures + f;
     float x = 0.f;
-    for (int i = r; i < n; i += 16) x += ws[(size_t)i * 2 * D + e];
+    for (int i0 = r; i0 < n; i0 += 8 * R) {
+        float y[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = i0 + i * R < n ? ws[(size_t)(i0 + i * R) * 2 * D + e] : 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x += y[i];
+    }
     part[r][f] = x;
     __syncthreads();
-    if (r != 0) return;
-    x = 0.f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) x += part[i][f];
+    for (int half = R / 2; half > 0; half /= 2) {
+        if (r < half) part[r][f] += part[r + half][f];
+        __syncthreads();
+    }
     float* out = e < D ? dgq : dgk;
-    if (out) out[e % D] = x;
+    if (r == 0 && out) out[e % D] = part[0][f];
 }
 
 }  // namespace
@@ -290,7 +339,7 @@ hipError_t launch_norm_rope_backward(const NormRopeParams& p, hipStream_t stream
         go(norm_rope_bwd_kernel<D, T, false>);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || (!p.gq && !p.gk)) return e;
-    hipLaunchKernelGGL((norm_rope_sum_kernel<D>), dim3(2 * D / 16), dim3(256), 0, stream, p.ws, wgs, p.dgq, p.dgk);
+    hipLaunchKernelGGL((norm_rope_sum_kernel<D>), dim3(2 * D / kSumFeatures), dim3(1024), 0, stream, p.ws, wgs, p.dgq, p.dgk);
     return hipGetLastError();
 }
 
