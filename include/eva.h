@@ -652,7 +652,8 @@ int eva_qcache_read(const eva_qcache* cache, const eva_rcache* to, void* stream)
 /* eva_rdecode_step, eva_rappend_decode (the append, then the decode: the row
  * reads its own token as the cache holds it) and eva_rtree_attention (drafted
  * tokens are read as they are given, in bf16) over an 8-bit cache; q and o
- * 16-byte aligned. */
+ * 16-byte aligned.  (Of an active sequence that holds no token the decode
+ * writes a row of zeros.) */
 int eva_qdecode_step(const eva_qcache* cache, const void* q, void* o, const int* active, void* ws, size_t ws_bytes,
                      void* stream);
 size_t eva_qdecode_workspace_bytes(const eva_qcache* cache);

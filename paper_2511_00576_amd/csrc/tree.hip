@@ -95,7 +95,13 @@ __global__ __launch_bounds__(NW * 64, NW == 12 ? 3 : 2) void tree_kernel(TreePar
     const int split = blockIdx.y;
     const CacheView& c = a.c;
     const TreeRows rows(a, unit / a.fHkv, DRAFT);
-    if (!rows.any) return;  // uniform across the workgroup
+    if (!rows.any) {  // uniform across the workgroup
+        // a row over nothing, of an active sequence without a token, is zero
+        if (!DRAFT && split == 0 && !(a.active && a.active[unit / a.fHkv] == 0))
+            for (int e = threadIdx.x; e < min(16, a.cols - cb * 16) * D; e += NW * 64)
+                static_cast<bf16*>(a.o)[((size_t)unit * a.cols + cb * 16) * D + e] = to_bf16(0.f);
+        return;
+    }
     const int n = rows.n, nodes = rows.nodes;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);

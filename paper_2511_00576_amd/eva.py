@@ -446,25 +446,33 @@ def prefill_backward(Q, K, V, Ks, Vs, O, lse, dO, W: int, C: int, workspace=None
 
 
 # ---- head norms with rotation ----------------------------------------------
-def _call(device, name, *args):
-    """Call lib.<name>(*args, stream) on `device`'s current stream, with that
-    device current."""
-    fn = getattr(_lib.load(), name)
-    if device.index == torch._C._cuda_getDevice():
-        _lib.check(name, fn(*args, _stream()))
+_functions = {}
+
+
+def _call(dev, name, *args):
+    """Call lib.<name>(*args, stream) on the current stream of device `dev` (its
+    index), with that device current."""
+    fn = _functions.get(name)
+    if fn is None:
+        fn = _functions[name] = getattr(_lib.load(), name)
+    if dev == torch._C._cuda_getDevice():
+        status = fn(*args, torch._C._cuda_getCurrentRawStream(dev))
     else:
-        with torch.cuda.device(device):
-            _lib.check(name, fn(*args, _stream()))
+        with torch.cuda.device(dev):
+            status = fn(*args, torch._C._cuda_getCurrentRawStream(dev))
+    if status != _lib.EVA_OK:
+        raise _lib.EvaError(name, status)
 
 
-def _expect(t, what, shape, dtype, device):
-    """An optional operand: contiguous, of this shape and dtype, on `device`."""
+def _expect(t, what, shape, dtype, dev):
+    """Address of an operand (None: no operand): contiguous, of this shape (a
+    tuple) and dtype, on device `dev`."""
     if t is None:
         return None
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+    if t.shape != shape or t.dtype is not dtype:
         raise ValueError(f"{what} must be {dtype} {list(shape)}")
-    if t.device != device:
-        raise RuntimeError(f"{what} must be on {device}")
+    if t.get_device() != dev:
+        raise RuntimeError(f"{what} must be on the same ROCm device as the others")
     if not t.is_contiguous():
         raise ValueError(f"{what} must be contiguous")
     return t.data_ptr()
@@ -483,22 +491,23 @@ def rope_turns(rot: int, base: float = 10000.0, inv_freq=None, device="cuda") ->
 
 
 def _norm_rope_args(x, H, Hkv, turns, q_weight, k_weight, eps, start, offsets, interleaved):
-    """The arguments both directions share, and (B, L, d)."""
-    if not x.is_cuda:
+    """The arguments both directions share, and (device, B, L, d)."""
+    dev = x.get_device()
+    if dev < 0:
         raise RuntimeError("EVA kernels run on the GPU only: tensors must be on a ROCm device")
     if x.dim() != 3 or H < 1 or Hkv < 1 or x.shape[2] % (H + 2 * Hkv) != 0:
         raise ValueError("x must be [B, L, (H + 2 Hkv) * d]")
-    if x.stride(2) != 1:
+    B, L, d = x.shape
+    d //= H + 2 * Hkv
+    sb, sl, sf = x.stride()
+    if sf != 1:
         raise ValueError("the features of x must be contiguous")
-    B, L, d = x.shape[0], x.shape[1], x.shape[2] // (H + 2 * Hkv)
-    # the stride of a single row is never used, and may be any number
-    sb, sl = x.stride(0) if B > 1 else 0, x.stride(1) if L > 1 else 0
     rot = 0 if turns is None else 2 * turns.numel()
-    return (_ptr(x), sb, sl, _expect(q_weight, "q_weight", (d,), x.dtype, x.device),
-            _expect(k_weight, "k_weight", (d,), x.dtype, x.device),
-            _expect(turns, "turns", (rot // 2,), torch.int64, x.device), rot, int(bool(interleaved)),
-            _expect(start, "start", (B,), torch.int32, x.device),
-            _expect(offsets, "offsets", (B, L), torch.int32, x.device), float(eps)), B, L, d
+    # the stride of a single row is never used, and may be any number
+    return (x.data_ptr(), sb if B > 1 else 0, sl if L > 1 else 0, _expect(q_weight, "q_weight", (d,), x.dtype, dev),
+            _expect(k_weight, "k_weight", (d,), x.dtype, dev), _expect(turns, "turns", (rot // 2,), torch.int64, dev),
+            rot, 1 if interleaved else 0, _expect(start, "start", (B,), torch.int32, dev),
+            _expect(offsets, "offsets", (B, L), torch.int32, dev), eps), dev, B, L, d
 
 
 def qk_norm_rope(x, H: int, Hkv: int, turns=None, q_weight=None, k_weight=None, eps: float = 1e-6, start=None,
@@ -511,17 +520,17 @@ def qk_norm_rope(x, H: int, Hkv: int, turns=None, q_weight=None, k_weight=None, 
     token's position is start[b] (int32 [B], a ragged cache's n_tok for one;
     None: 0) + offsets[b, l] (int32 [B, L]; None: l).  `out` = (Q, K, V)
     preallocated."""
-    args, B, L, d = _norm_rope_args(x, H, Hkv, turns, q_weight, k_weight, eps, start, offsets, interleaved)
+    args, dev, B, L, d = _norm_rope_args(x, H, Hkv, turns, q_weight, k_weight, eps, start, offsets, interleaved)
+    code = _dtype_code(x)
     if out is None:
-        Q = torch.empty(B, H, L, d, dtype=x.dtype, device=x.device)
-        K, V = (torch.empty(B, Hkv, L, d, dtype=x.dtype, device=x.device) for _ in range(2))
+        Q, K, V = x.new_empty((B, H, L, d)), x.new_empty((B, Hkv, L, d)), x.new_empty((B, Hkv, L, d))
+        q, k, v = Q.data_ptr(), K.data_ptr(), V.data_ptr()
     else:
         Q, K, V = out
-    if B == 0 or L == 0:
-        return Q, K, V
-    _call(x.device, "eva_qk_norm_rope", *args, _expect(Q, "Q", (B, H, L, d), x.dtype, x.device),
-          _expect(K, "K", (B, Hkv, L, d), x.dtype, x.device), _expect(V, "V", (B, Hkv, L, d), x.dtype, x.device), B, H,
-          Hkv, L, d, _dtype_code(x))
+        q = _expect(Q, "Q", (B, H, L, d), x.dtype, dev)
+        k, v = (_expect(t, "K and V", (B, Hkv, L, d), x.dtype, dev) for t in (K, V))
+    if B > 0 and L > 0:
+        _call(dev, "eva_qk_norm_rope", *args, q, k, v, B, H, Hkv, L, d, code)
     return Q, K, V
 
 
@@ -530,21 +539,25 @@ def qk_norm_rope_backward(x, dQ, dK, dV, turns=None, q_weight=None, k_weight=Non
     """Gradients of qk_norm_rope: dQ [B, H, L, d], dK, dV [B, Hkv, L, d] ->
     (dx [B, L, (H + 2 Hkv) * d], dq_weight, dk_weight), the weights' in fp32
     (None where there is no weight)."""
+    if dQ.dim() != 4 or dK.dim() != 4:
+        raise ValueError("dQ [B, H, L, d], dK and dV [B, Hkv, L, d] expected")
     H, Hkv = dQ.shape[1], dK.shape[1]
-    args, B, L, d = _norm_rope_args(x, H, Hkv, turns, q_weight, k_weight, eps, start, offsets, interleaved)
-    grads = (_expect(dQ, "dQ", (B, H, L, d), x.dtype, x.device), _expect(dK, "dK", (B, Hkv, L, d), x.dtype, x.device),
-             _expect(dV, "dV", (B, Hkv, L, d), x.dtype, x.device))
-    dx = torch.empty(B, L, x.shape[2], dtype=x.dtype, device=x.device)
-    new = torch.zeros if B == 0 or L == 0 else torch.empty
-    dg = [None if w is None else new(d, dtype=torch.float32, device=x.device) for w in (q_weight, k_weight)]
-    if B == 0 or L == 0:
+    args, dev, B, L, d = _norm_rope_args(x, H, Hkv, turns, q_weight, k_weight, eps, start, offsets, interleaved)
+    code = _dtype_code(x)
+    grads = (_expect(dQ, "dQ", (B, H, L, d), x.dtype, dev), _expect(dK, "dK", (B, Hkv, L, d), x.dtype, dev),
+             _expect(dV, "dV", (B, Hkv, L, d), x.dtype, dev))
+    dx = x.new_empty(x.shape)
+    none = B == 0 or L == 0
+    dg = [None if w is None else (x.new_zeros if none else x.new_empty)(d, dtype=torch.float32)
+          for w in (q_weight, k_weight)]
+    if none:
         return (dx, *dg)
-    ws = None
+    n = ws = 0
     if q_weight is not None or k_weight is not None:
         n = _lib.load().eva_qk_norm_rope_backward_workspace_bytes(B, L, d)
-        ws = torch.empty((n + 3) // 4, dtype=torch.float32, device=x.device)
-    _call(x.device, "eva_qk_norm_rope_backward", *args, *grads, _ptr(dx), _ptr(dg[0]), _ptr(dg[1]), _ptr(ws),
-          ws.numel() * 4 if ws is not None else 0, B, H, Hkv, L, d, _dtype_code(x))
+        ws = x.new_empty(n, dtype=torch.uint8)
+    _call(dev, "eva_qk_norm_rope_backward", *args, *grads, dx.data_ptr(), _ptr(dg[0]), _ptr(dg[1]),
+          ws.data_ptr() if n else None, n, B, H, Hkv, L, d, code)
     return (dx, *dg)
 
 
@@ -591,49 +604,39 @@ class QuantCache:
         return int(self.struct.S_max)
 
 
-def _of_cache(cache, t, what, shape):
-    """An operand in the cache's dtype, contiguous and on its device."""
-    return _expect(t, what, shape, cache.dtype, cache.n_tok.device)
-
-
-def _ints(cache, t, what, shape):
-    return _expect(t, what, shape, torch.int32, cache.n_tok.device)
-
-
-def _scratch(cache, n):
-    """(pointer, bytes, tensor) of a workspace of n bytes."""
-    if n == 0:
-        return None, 0, None
-    ws = torch.empty((n + 3) // 4, dtype=torch.float32, device=cache.n_tok.device)
-    return ws.data_ptr(), n, ws
-
-
-def _rows_out(cache, q, out, whole):
+def _rows_out(q, out, whole, dev):
     """The output of q's shape: `out`, or a new one (zeros where the call may
-    leave rows unwritten)."""
+    leave rows unwritten); and its address."""
     if out is None:
-        return torch.empty_like(q) if whole else torch.zeros_like(q)
-    _of_cache(cache, out, "out", q.shape)
-    return out
+        out = torch.empty_like(q) if whole else torch.zeros_like(q)
+        return out, out.data_ptr()
+    return out, _expect(out, "out", q.shape, q.dtype, dev)
+
+
+def _scratch(q, n):
+    """A workspace of n bytes of the call's own (None: none needed)."""
+    return q.new_empty(n, dtype=torch.uint8) if n else None
 
 
 def qcache_fill(cache: QuantCache, K, V, Ks, Vs, lens):
     """rcache_fill into an 8-bit cache: K, V [B, Hkv, L, d] and their summaries,
     quantised; lens (int32 [B]) are the valid lengths."""
-    s = cache.struct
-    B, Hkv, L, d = K.shape
+    s, dev, dt = cache.struct, cache.n_tok.get_device(), cache.dtype
+    if K.dim() != 4:
+        raise ValueError("K must be [B, Hkv, L, d]")
+    L = K.shape[2]
     shape, sums = (s.B, s.H_kv, L, s.d), (s.B, s.H_kv, L // s.C, s.d)
-    _call(cache.n_tok.device, "eva_qcache_fill", ctypes.byref(s), _of_cache(cache, K, "K", shape),
-          _of_cache(cache, V, "V", shape), _of_cache(cache, Ks, "Ks", sums), _of_cache(cache, Vs, "Vs", sums), L,
-          _ints(cache, lens, "lens", (s.B,)))
+    _call(dev, "eva_qcache_fill", ctypes.byref(s), _expect(K, "K", shape, dt, dev), _expect(V, "V", shape, dt, dev),
+          _expect(Ks, "Ks", sums, dt, dev), _expect(Vs, "Vs", sums, dt, dev), L,
+          _expect(lens, "lens", (s.B,), torch.int32, dev))
 
 
 def qcache_append(cache: QuantCache, k_new, v_new, active=None):
     """Append one token to each active sequence: k_new, v_new [B, Hkv, d]."""
-    s = cache.struct
+    s, dev, dt = cache.struct, cache.n_tok.get_device(), cache.dtype
     row = (s.B, s.H_kv, s.d)
-    _call(cache.n_tok.device, "eva_qcache_append", ctypes.byref(s), _of_cache(cache, k_new, "k_new", row),
-          _of_cache(cache, v_new, "v_new", row), _ints(cache, active, "active", (s.B,)))
+    _call(dev, "eva_qcache_append", ctypes.byref(s), _expect(k_new, "k_new", row, dt, dev),
+          _expect(v_new, "v_new", row, dt, dev), _expect(active, "active", (s.B,), torch.int32, dev))
 
 
 def qcache_read(cache: QuantCache, to: RaggedCache) -> RaggedCache:
@@ -641,35 +644,32 @@ def qcache_read(cache: QuantCache, to: RaggedCache) -> RaggedCache:
     `to` of the same geometry, which can then go on with them."""
     if to.n_tok.device != cache.n_tok.device:
         raise RuntimeError("both caches must be on one device")
-    _call(cache.n_tok.device, "eva_qcache_read", ctypes.byref(cache.struct), ctypes.byref(to.struct))
+    _call(cache.n_tok.get_device(), "eva_qcache_read", ctypes.byref(cache.struct), ctypes.byref(to.struct))
     return to
+
+
+def _qdecode(cache, name, q, new, active, out, use_workspace):
+    s, dev, dt = cache.struct, cache.n_tok.get_device(), cache.dtype
+    args = [_expect(q, "q", (s.B, s.H, s.d), dt, dev)]
+    args += [_expect(t, "k_new and v_new", (s.B, s.H_kv, s.d), dt, dev) for t in new]
+    on = _expect(active, "active", (s.B,), torch.int32, dev)
+    o, po = _rows_out(q, out, active is None, dev)
+    n = _lib.load().eva_qdecode_workspace_bytes(ctypes.byref(s)) if use_workspace else 0
+    ws = _scratch(q, n)
+    _call(dev, name, ctypes.byref(s), *args, po, on, _ptr(ws), n)
+    return o
 
 
 def qdecode_step(cache: QuantCache, q, active=None, out=None, use_workspace=True):
     """rdecode_step over an 8-bit cache: q [B, H, d] -> o [B, H, d].  Rows of
-    inactive or empty sequences keep the contents of `out`."""
-    s = cache.struct
-    qp = _of_cache(cache, q, "q", (s.B, s.H, s.d))
-    o = _rows_out(cache, q, out, False)
-    n = _lib.load().eva_qdecode_workspace_bytes(ctypes.byref(s)) if use_workspace else 0
-    wp, nbytes, ws = _scratch(cache, n)
-    _call(cache.n_tok.device, "eva_qdecode_step", ctypes.byref(s), qp, _ptr(o), _ints(cache, active, "active", (s.B,)),
-          wp, nbytes)
-    return o
+    inactive sequences keep the contents of `out`, those of empty ones are
+    zeros."""
+    return _qdecode(cache, "eva_qdecode_step", q, (), active, out, use_workspace)
 
 
 def qappend_decode(cache: QuantCache, q, k_new, v_new, active=None, out=None, use_workspace=True):
     """qcache_append(k_new, v_new), then qdecode_step(q)."""
-    s = cache.struct
-    row = (s.B, s.H_kv, s.d)
-    args = (_of_cache(cache, q, "q", (s.B, s.H, s.d)), _of_cache(cache, k_new, "k_new", row),
-            _of_cache(cache, v_new, "v_new", row))
-    o = _rows_out(cache, q, out, False)
-    n = _lib.load().eva_qdecode_workspace_bytes(ctypes.byref(s)) if use_workspace else 0
-    wp, nbytes, ws = _scratch(cache, n)
-    _call(cache.n_tok.device, "eva_qappend_decode", ctypes.byref(s), *args, _ptr(o),
-          _ints(cache, active, "active", (s.B,)), wp, nbytes)
-    return o
+    return _qdecode(cache, "eva_qappend_decode", q, (k_new, v_new), active, out, use_workspace)
 
 
 # ---- drafted trees -----------------------------------------------------------
@@ -682,19 +682,23 @@ def tree_attention(cache, q, k, v, parents, n_nodes=None, active=None, out=None,
     sequence itself.  n_nodes (int32 [B]): each tree's size, T if None.  Node t's
     position is n_tok[b] + its depth.  T is at most 64 and W.  Rows of inactive
     sequences and absent nodes keep the contents of `out`."""
-    s = cache.struct
+    s, dev, dt = cache.struct, cache.n_tok.get_device(), cache.dtype
     if q.dim() != 4:
         raise ValueError("q must be [B, H, T, d]")
-    T = q.shape[2]
-    row = (s.B, s.H_kv, T, s.d)
-    args = (_of_cache(cache, q, "q", (s.B, s.H, T, s.d)), _of_cache(cache, k, "k", row), _of_cache(cache, v, "v", row),
-            _ints(cache, parents, "parents", (s.B, T)), _ints(cache, n_nodes, "n_nodes", (s.B,)))
-    o = _rows_out(cache, q, out, n_nodes is None and active is None)
-    kind = "eva_q" if isinstance(cache, QuantCache) else "eva_r"
-    n = getattr(_lib.load(), kind + "tree_workspace_bytes")(ctypes.byref(s), T) if use_workspace else 0
-    wp, nbytes, ws = _scratch(cache, n)
-    _call(cache.n_tok.device, kind + "tree_attention", ctypes.byref(s), *args, _ptr(o), T,
-          _ints(cache, active, "active", (s.B,)), wp, nbytes)
+    T, B, d = q.shape[2], s.B, s.d
+    row = (B, s.H_kv, T, d)
+    args = (_expect(q, "q", (B, s.H, T, d), dt, dev), _expect(k, "k", row, dt, dev), _expect(v, "v", row, dt, dev),
+            _expect(parents, "parents", (B, T), torch.int32, dev), _expect(n_nodes, "n_nodes", (B,), torch.int32, dev))
+    on = _expect(active, "active", (B,), torch.int32, dev)
+    o, po = _rows_out(q, out, n_nodes is None and active is None, dev)
+    ref, lib = ctypes.byref(s), _lib.load()
+    if isinstance(cache, QuantCache):
+        name, size = "eva_qtree_attention", lib.eva_qtree_workspace_bytes
+    else:
+        name, size = "eva_rtree_attention", lib.eva_rtree_workspace_bytes
+    n = size(ref, T) if use_workspace else 0
+    ws = _scratch(q, n)
+    _call(dev, name, ref, *args, po, T, on, _ptr(ws), n)
     return o
 
 
@@ -702,12 +706,11 @@ def append_path(cache, k, v, path=None, counts=None, active=None):
     """Append an accepted path to every active sequence of a RaggedCache or
     QuantCache: the tokens path[b, :counts[b]] (int32 [B, T], [B]; by default
     all T in their order) of k, v [B, Hkv, T, d]."""
-    s = cache.struct
+    s, dev, dt = cache.struct, cache.n_tok.get_device(), cache.dtype
     if k.dim() != 4:
         raise ValueError("k must be [B, Hkv, T, d]")
-    T = k.shape[2]
-    row = (s.B, s.H_kv, T, s.d)
-    _call(cache.n_tok.device, ("eva_q" if isinstance(cache, QuantCache) else "eva_r") + "append_path",
-          ctypes.byref(s), _of_cache(cache, k, "k", row), _of_cache(cache, v, "v", row),
-          _ints(cache, path, "path", (s.B, T)), _ints(cache, counts, "counts", (s.B,)), T,
-          _ints(cache, active, "active", (s.B,)))
+    T, B = k.shape[2], s.B
+    row = (B, s.H_kv, T, s.d)
+    _call(dev, "eva_qappend_path" if isinstance(cache, QuantCache) else "eva_rappend_path", ctypes.byref(s),
+          _expect(k, "k", row, dt, dev), _expect(v, "v", row, dt, dev), _expect(path, "path", (B, T), torch.int32, dev),
+          _expect(counts, "counts", (B,), torch.int32, dev), T, _expect(active, "active", (B,), torch.int32, dev))
