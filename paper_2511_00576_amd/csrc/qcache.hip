@@ -64,17 +64,28 @@ __global__ __launch_bounds__(256) void qcache_fill_kernel(QCacheView c, const bf
     }
     if (r0 >= r1) return;  // the same for the whole workgroup
     const int cc = threadIdx.x % TPR;
+    // all of the thread's pieces before any wait (rows that are not the tile's:
+    // its first again)
+    constexpr int NS = kQFillRows / RPS;
+    u32x4 kw[NS], vw[NS];
 #pragma unroll
-    for (int s = 0; s < kQFillRows / RPS; ++s) {
+    for (int s = 0; s < NS; ++s) {
+        const int row = t0 + s * RPS + (int)threadIdx.x / TPR;
+        const size_t at = (size_t)(row < r0 || row >= r1 ? r0 : row) * D + cc * 8;
+        kw[s] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src_k + at));
+        vw[s] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src_v + at));
+    }
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
         const int i = s * RPS + (int)threadIdx.x / TPR;
         const int row = t0 + i;
         if (row < r0 || row >= r1) continue;  // a row's lanes stay together
         float x[8];
         u32x2 codes;
-        row8(src_k + (size_t)row * D + cc * 8, x);
+        unpack8(kw[s], x);
         const uint32_t ke = q_row<D>(x, codes);
         *reinterpret_cast<u32x2*>(dst_k + (size_t)(slot0 + i) * D + cc * 8) = codes;
-        row8(src_v + (size_t)row * D + cc * 8, x);
+        unpack8(vw[s], x);
         const uint32_t ve = q_row<D>(x, codes);
         *reinterpret_cast<uint32_t*>(vcodes + i * kStride + cc * 8) = codes[0];
         *reinterpret_cast<uint32_t*>(vcodes + i * kStride + cc * 8 + 4) = codes[1];
@@ -118,6 +129,101 @@ __global__ __launch_bounds__(256) void qcache_fill_kernel(QCacheView c, const bf
 // ---------------------------------------------------------------------------
 // append of a path
 // ---------------------------------------------------------------------------
+// The summary of a chunk of the 8-bit ring, chunk_summary's in its own layout:
+// keys in batches of four rows a thread (requested together: one after the
+// other, each sweep waits for memory), values by 16 slots of a feature a load.
+// Threads t < D / 8 are left with features 8t .. of both rows.
+template <int D>
+__device__ void q_chunk_summary(const QRingChunk<D>& src, int C, float* logits, float* red, float khat[8], float vhat[8]) {
+    constexpr int TPR = D / 8, RPS = kSummaryThreads / TPR, NB = 4;
+    const int t = threadIdx.x, cc = t % TPR, r0 = t / TPR;
+    // rows r, r + RPS, ..: their features cc 8 .. times their scale
+    auto keys = [&](int r, float (&k)[NB][8]) {
+        u32x2 w[NB];
+        uint32_t x[NB];
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+            const int s = src.slot(min(r + i * RPS, C - 1));
+            w[i] = *reinterpret_cast<const u32x2*>(src.k + (size_t)s * D + cc * 8);
+            x[i] = src.ke[s];
+        }
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) k[i][e] = q_value(w[i][e >> 2] >> (8 * (e & 3)), q_scale(x[i]));
+    };
+    float ks[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    for (int r = r0; r < C; r += NB * RPS) {
+        float k[NB][8];
+        keys(r, k);
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+            if (r + i * RPS < C)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) ks[e] += k[i][e];
+    }
+    reduce_rows8<TPR>(ks, red);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) khat[e] = ks[e] * (1.0f / (float)C);
+
+    const float sc = kLog2e * rsqrtf((float)D);
+    float amax = -INFINITY;
+    for (int r = r0; r < C; r += NB * RPS) {
+        float k[NB][8];
+        keys(r, k);
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+            float s = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s += khat[e] * k[i][e];
+#pragma unroll
+            for (int off = 1; off < TPR; off <<= 1) s += __shfl_xor(s, off, 64);
+            s *= sc;
+            if (r + i * RPS < C) {
+                if (cc == 0) logits[r + i * RPS] = s;
+                amax = fmaxf(amax, s);
+            }
+        }
+    }
+    amax = block_max(amax, red);  // also orders the logits' writes before their reads
+
+    // thread's feature and its share of the 16-slot tiles that the chunk touches
+    constexpr int TG = kSummaryThreads / D;
+    const int f = t % D;
+    const long long p16 = src.pos0 & ~15ll;
+    const int tiles = (int)((src.pos0 + C - 1 - p16) / 16) + 1;
+    float acc = 0.f, den = 0.f;
+    for (int i = t / D; i < tiles; i += TG) {
+        const int s = (int)((p16 + 16 * i) % src.R);
+        const u32x4 w = *reinterpret_cast<const u32x4*>(src.vt + qt_index<D>(f, s));
+        const u32x4 x = *reinterpret_cast<const u32x4*>(src.ve + s);
+        const int row = (int)(p16 - src.pos0) + 16 * i;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            if ((unsigned)(row + j) >= (unsigned)C) continue;  // another chunk's row
+            const float p = fast_exp2(logits[row + j] - amax);
+            den += p;
+            acc += p * q_value(w[j >> 2] >> (8 * (j & 3)), q_scale(x[j >> 2] >> (8 * (j & 3)) & 255));
+        }
+    }
+    __syncthreads();  // block_max's reads of red are done
+    red[t] = acc;
+    red[kSummaryThreads + t] = den;
+    __syncthreads();
+    if (t < TPR) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            float a = 0.f, d = 0.f;
+#pragma unroll
+            for (int g = 0; g < TG; ++g) {
+                a += red[g * D + 8 * t + e];
+                d += red[kSummaryThreads + g * D + 8 * t + e];
+            }
+            vhat[e] = a / d;
+        }
+    }
+}
+
 // One workgroup per (b, kv head).  The path's tokens take positions n, n + 1,
 // ... : all their rows are written first, then the chunks they complete are
 // summarised from the ring (which holds every position of such a chunk: R >=
@@ -248,7 +354,10 @@ __global__ __launch_bounds__(kSummaryThreads) void append_path_kernel(View c, Pa
                 continue;
             }
         }
-        chunk_summary<D>(store.chunk(s), c.C, smem, smem + c.C, kh, vh);
+        if constexpr (std::is_same<View, QCacheView>::value)
+            q_chunk_summary<D>(store.chunk(s), c.C, smem, smem + c.C, kh, vh);
+        else
+            chunk_summary<D>(store.chunk(s), c.C, smem, smem + c.C, kh, vh);
         store.summary(bg, s, kh, vh);
     }
     if (threadIdx.x == 0) {
@@ -264,7 +373,10 @@ __global__ __launch_bounds__(kSummaryThreads) void append_path_kernel(View c, Pa
 // ---------------------------------------------------------------------------
 // One workgroup per 32 rows (32 ring positions, 32-aligned, or 32 summaries):
 // keys row by row, values feature by feature (16 slots in, two of the bf16
-// cache's 8-slot pieces out), all in registers.
+// cache's 8-slot pieces out), all in registers.  Non-temporal stores: 25.8 us for
+// 137 MB instead of 29.3 (64 x 8 heads x 352 rows of 128 features; 64 rows a
+// workgroup 27.6).
+constexpr int kQReadRows = 32;
 template <int D>
 __global__ __launch_bounds__(256) void qcache_read_kernel(QCacheView c, CacheView to, const int* __restrict__ n_tok,
                                                           int max_tok, RaggedState rs, int ring_tiles) {
@@ -315,8 +427,8 @@ __global__ __launch_bounds__(256) void qcache_read_kernel(QCacheView c, CacheVie
         for (int j = 0; j < 8; ++j)
             out[j] = pack_bf16x2(q_value(w[j >> 1] >> (16 * (j & 1)), sc), q_value(w[j >> 1] >> (16 * (j & 1) + 8), sc));
         u32x4* dst = reinterpret_cast<u32x4*>(ok + (size_t)(dst0 + i) * D + f);
-        dst[0] = u32x4{out[0], out[1], out[2], out[3]};
-        dst[1] = u32x4{out[4], out[5], out[6], out[7]};
+        __builtin_nontemporal_store(u32x4{out[0], out[1], out[2], out[3]}, dst);
+        __builtin_nontemporal_store(u32x4{out[4], out[5], out[6], out[7]}, dst + 1);
     }
     for (int e = threadIdx.x; e < 2 * D; e += 256) {
         const int f = e % D, g = e / D * kQTile;
@@ -333,7 +445,7 @@ __global__ __launch_bounds__(256) void qcache_read_kernel(QCacheView c, CacheVie
             const int i0 = g + 8 * h;
             bf16* dst = ovt + vt_index<D>(f, dst0 + i0);
             if (t0 + i0 >= r0 && t0 + i0 + 8 <= r1) {
-                *reinterpret_cast<u32x4*>(dst) = u32x4{out[4 * h], out[4 * h + 1], out[4 * h + 2], out[4 * h + 3]};
+                __builtin_nontemporal_store(u32x4{out[4 * h], out[4 * h + 1], out[4 * h + 2], out[4 * h + 3]}, reinterpret_cast<u32x4*>(dst));
             } else {
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
@@ -363,8 +475,8 @@ template <int D>
 hipError_t launch_qcache_read(const QCacheView& c, const CacheView& to, const int* n_tok, int max_tok,
                               const RaggedState& r, hipStream_t stream) {
     const int most = min(max_tok, r.max_tok);
-    const int ring_tiles = min(most, min(c.R, to.R)) / 32 + 2;
-    const int sum_tiles = (min(most / c.C, min(c.S_max, to.S_max)) + 31) / 32;
+    const int ring_tiles = (min(most, min(c.R, to.R)) + kQReadRows - 1) / kQReadRows + 1;
+    const int sum_tiles = (min(most / c.C, min(c.S_max, to.S_max)) + kQReadRows - 1) / kQReadRows;
     hipLaunchKernelGGL((qcache_read_kernel<D>), dim3(ring_tiles + sum_tiles, c.B * c.Hkv), dim3(256), 0, stream, c, to,
                        n_tok, max_tok, r, ring_tiles);
     return hipGetLastError();
@@ -379,7 +491,8 @@ hipError_t launch_append_path(const CacheView& c, const PathParams& a, hipStream
 }
 template <int D>
 hipError_t launch_qappend_path(const QCacheView& c, const PathParams& a, hipStream_t stream) {
-    const size_t lds = (size_t)(c.C + summary_red_floats<D>()) * sizeof(float);
+    constexpr int red = summary_red_floats<D>() > 2 * kSummaryThreads ? summary_red_floats<D>() : 2 * kSummaryThreads;
+    const size_t lds = (size_t)(c.C + red) * sizeof(float);
     hipLaunchKernelGGL((append_path_kernel<D, bf16, QuantStore<D>, QCacheView>), dim3(c.B * c.Hkv), dim3(kSummaryThreads), lds,
                        stream, c, a);
     return hipGetLastError();

@@ -78,17 +78,17 @@ __device__ __forceinline__ bf16x8 q_bf16x8(uint32_t lo, uint32_t hi) {
     return __builtin_bit_cast(bf16x8, u32x4{q_bf16x2<false>(lo), q_bf16x2<true>(lo), q_bf16x2<false>(hi), q_bf16x2<true>(hi)});
 }
 
-// Eight features of a row of T as fp32.
-__device__ __forceinline__ void row8(const bf16* p, float out[8]) {
-    const u32x4 w = *reinterpret_cast<const u32x4*>(p);
+// Eight bf16 features as fp32.
+__device__ __forceinline__ void unpack8(const u32x4& w, float out[8]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         out[2 * i] = bf16_lo(w[i]);
         out[2 * i + 1] = bf16_hi(w[i]);
     }
 }
+__device__ __forceinline__ void row8(const bf16* p, float out[8]) { unpack8(*reinterpret_cast<const u32x4*>(p), out); }
 
-// Rows of a chunk in the 8-bit ring (the source of chunk_summary).
+// Rows of a chunk in the 8-bit ring.
 template <int D>
 struct QRingChunk {
     const uint8_t* k;   // this (b, g): [R][D]
@@ -98,19 +98,6 @@ struct QRingChunk {
     long long pos0;
     int R;
     __device__ int slot(int r) const { return (int)((pos0 + r) % R); }
-    __device__ void load_k(int r, int cc, float out[8]) const {
-        const int s = slot(r);
-        const u32x2 w = *reinterpret_cast<const u32x2*>(k + (size_t)s * D + cc * 8);
-        const float sc = q_scale(ke[s]);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) out[i] = q_value(w[i >> 2] >> (8 * (i & 3)), sc);
-    }
-    __device__ void load_v(int r, int cc, float out[8]) const {
-        const int s = slot(r);
-        const float sc = q_scale(ve[s]);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) out[i] = q_value(vt[qt_index<D>(cc * 8 + i, s)], sc);
-    }
 };
 
 }  // namespace eva

@@ -94,7 +94,21 @@ __global__ __launch_bounds__(NW * 64, NW == 12 ? 3 : 2) void tree_kernel(TreePar
     if (unit >= a.units) return;
     const int split = blockIdx.y;
     const CacheView& c = a.c;
-    const TreeRows rows(a, unit / a.fHkv, DRAFT);
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int g = lane >> 4, c16 = lane & 15;
+    const size_t bg = (size_t)unit;
+
+    // Column c16 (past the last: the last again; a column's results depend on it
+    // alone, and theirs are not stored), its query's features 32 dc + 8 g ..
+    // (8-bit: 64 (dc / 2) + 16 g + 8 (dc % 2) .., both halves of a 16-byte read).
+    const int col = min(cb * 16 + c16, a.cols - 1);
+    auto feature = [&](int dc) { return Q8 ? 64 * (dc >> 1) + 16 * g + 8 * (dc & 1) : 32 * dc + 8 * g; };
+    bf16x8 qf[NDC];
+#pragma unroll
+    for (int dc = 0; dc < NDC; ++dc)
+        qf[dc] = *reinterpret_cast<const bf16x8*>(static_cast<const bf16*>(a.q) + (bg * a.cols + col) * D + feature(dc));
+    const TreeRows rows(a, unit / a.fHkv, DRAFT);  // (the queries' loads are in flight meanwhile)
     if (!rows.any) {  // uniform across the workgroup
         // a row over nothing, of an active sequence without a token, is zero
         if (!DRAFT && split == 0 && !(a.active && a.active[unit / a.fHkv] == 0))
@@ -103,10 +117,6 @@ __global__ __launch_bounds__(NW * 64, NW == 12 ? 3 : 2) void tree_kernel(TreePar
         return;
     }
     const int n = rows.n, nodes = rows.nodes;
-    const int tid = threadIdx.x, lane = tid & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int g = lane >> 4, c16 = lane & 15;
-    const size_t bg = (size_t)unit;
 
     // drafted values: rows into LDS
     bf16* vdraft = reinterpret_cast<bf16*>(tree_smem);
@@ -121,18 +131,9 @@ __global__ __launch_bounds__(NW * 64, NW == 12 ? 3 : 2) void tree_kernel(TreePar
         }
     }
 
-    // Column c16 (past the last: the last again; a column's results depend on it
-    // alone, and theirs are not stored), its query's features 32 dc + 8 g ..
-    // (8-bit: 64 (dc / 2) + 16 g + 8 (dc % 2) .., both halves of a 16-byte read).
-    const int col = min(cb * 16 + c16, a.cols - 1);
     unsigned long long line;
     int lo, n_sum;
     rows.node(a, DRAFT ? col % a.fT : 0, line, lo, n_sum);
-    auto feature = [&](int dc) { return Q8 ? 64 * (dc >> 1) + 16 * g + 8 * (dc & 1) : 32 * dc + 8 * g; };
-    bf16x8 qf[NDC];
-#pragma unroll
-    for (int dc = 0; dc < NDC; ++dc)
-        qf[dc] = *reinterpret_cast<const bf16x8*>(static_cast<const bf16*>(a.q) + (bg * a.cols + col) * D + feature(dc));
     floatx4 acc[NDB];  // features db*16 + 4g .. +3
 #pragma unroll
     for (int db = 0; db < NDB; ++db) acc[db] = floatx4{0.f, 0.f, 0.f, 0.f};

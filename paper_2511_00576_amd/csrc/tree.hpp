@@ -10,15 +10,16 @@ constexpr float kTreeTau = 8.f;  // log2 units: unscaled weights stay <= 256
 constexpr int kMaxNodes = 64;
 
 // Lines of the tree's nodes: lane t holds the set of node t's forerunners and
-// itself.  Parents name an earlier node; any other value makes a root.  Six
-// rounds of doubling reach 64 nodes back.
-// parent: lane t's entry of the parents.
-__device__ __forceinline__ unsigned long long tree_lines(int parent, int nodes) {
+// itself.  parent: lane t's entry of the parents; they name an earlier node, any
+// other value makes a root.  Each round doubles the reach, until every line has
+// its root: `deepest` is a bound on the nodes' depths, below twice the largest.
+__device__ __forceinline__ unsigned long long tree_lines(int parent, int nodes, int& deepest) {
     const int lane = threadIdx.x & 63;
     int up = lane < nodes && parent >= 0 && parent < lane ? parent : -1;
     unsigned long long line = 1ull << lane;
-#pragma unroll
-    for (int r = 0; r < 6; ++r) {
+    int reach = 1;
+#pragma unroll 1
+    while (__builtin_amdgcn_ballot_w64(up >= 0)) {  // six rounds at most: up < lane
         const int from = max(up, 0);
         const unsigned long long l = __shfl(line, from, 64);
         const int u = __shfl(up, from, 64);
@@ -26,12 +27,14 @@ __device__ __forceinline__ unsigned long long tree_lines(int parent, int nodes) 
             line |= l;
             up = u;
         }
+        reach *= 2;
     }
+    deepest = min(reach, nodes) - 1;
     return line;
 }
 
 // A sequence's rows: the first ring position and the visible summaries of the
-// shallowest and of the deepest node, and of single nodes.  A plain decode
+// shallowest and of the deepest node there may be, and of single nodes.  A plain decode
 // (drafted false) is one node at the last position.
 struct TreeRows {
     int n, nodes;              // tokens held, nodes there are
@@ -52,11 +55,7 @@ struct TreeRows {
         if (!any) return;
         int deepest = 0;
         if (drafted) {
-            lines = tree_lines(parent, nodes);
-            deepest = lane < nodes ? __builtin_popcountll(lines) - 1 : 0;
-#pragma unroll
-            for (int off = 1; off < 64; off <<= 1) deepest = max(deepest, __shfl_xor(deepest, off, 64));
-            deepest = __builtin_amdgcn_readfirstlane(deepest);
+            lines = tree_lines(parent, nodes, deepest);
         }
         lo_first = win_lo_rt(a.c.window, p0, a.c.W, a.c.C);
         lo_last = win_lo_rt(a.c.window, p0 + deepest, a.c.W, a.c.C);

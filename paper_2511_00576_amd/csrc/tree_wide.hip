@@ -66,12 +66,14 @@ __device__ __forceinline__ void stream_reads(Load&& load, Use&& use) {
     u32x4 op[kFragAhead + 1];
 #pragma unroll
     for (int k = 0; k < kFragAhead && k < N; ++k) op[k] = load(k);
+    __builtin_amdgcn_s_setprio(1);  // the products first
 #pragma unroll
     for (int k = 0; k < N; ++k) {
         if (k + kFragAhead < N) op[(k + kFragAhead) % (kFragAhead + 1)] = load(k + kFragAhead);
         use(k, op[k % (kFragAhead + 1)]);
         __builtin_amdgcn_sched_barrier(0);
     }
+    __builtin_amdgcn_s_setprio(0);
 }
 
 template <int D, bool Q8, int WC>
@@ -89,14 +91,25 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(TreeParams a) {
     const int unit = place.unit, cb = place.cb;
     if (unit >= a.units) return;
     const CacheView& c = a.c;
-    const TreeRows rows(a, unit / a.fHkv, true);
-    if (!rows.any) return;  // uniform across the workgroup
-    const int n = rows.n, nodes = rows.nodes, split = blockIdx.y;
     const size_t bg = (size_t)unit;
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wc = wave % WC, wk = wave / WC;
     const int c32 = lane & 31, h2 = lane >> 5;
+
+    // ---- the wave's columns (their loads are in flight while the tree is read) ----
+    const int col0 = (cb * WC + wc) * 32;
+    const int col = min(col0 + c32, a.cols - 1);  // past the last: the last again, not stored
+    bf16x8 qf[NDC];  // features 16 dc + 8 h2 ..; 8-bit: step 2p + e has 32 p + 16 h2 + 8 e ..
+    {
+        const bf16* q = static_cast<const bf16*>(a.q) + (bg * a.cols + col) * D;
+#pragma unroll
+        for (int dc = 0; dc < NDC; ++dc)
+            qf[dc] = *reinterpret_cast<const bf16x8*>(q + (Q8 ? 32 * (dc >> 1) + 16 * h2 + 8 * (dc & 1) : 16 * dc + 8 * h2));
+    }
+    const TreeRows rows(a, unit / a.fHkv, true);
+    if (!rows.any) return;  // uniform across the workgroup
+    const int n = rows.n, nodes = rows.nodes, split = blockIdx.y;
 
     // ---- the blocks ----
     const int sum_blocks = (rows.sum_last + T::KEYS - 1) / T::KEYS;
@@ -114,18 +127,15 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(TreeParams a) {
     }();
     const unsigned v_off = wave * 1024 + lane * 16;
     const unsigned dk_off = dma_lane_off<D, true>(wave, lane), dv_off = dma_lane_off<D, false>(wave, lane);
-    // first row of cache block j in its array, its position (or summary)
-    auto cache_row = [&](int j, int& pos) {
-        if (j < sum_blocks) return pos = j * T::KEYS;
-        pos = (win0 + j - sum_blocks) * T::KEYS;
-        return pos % c.R;
-    };
+    // ring slot of the next window block that is requested (blocks are requested in
+    // their order: a division once)
+    int slot = (win0 + max(j0 - sum_blocks, 0)) * T::KEYS % c.R;
     auto request = [&](int j, int stage) {
         const unsigned base = lds0 + stage * Stage::BYTES;
         if (j < cache_blocks || j >= j1) {
             const bool sum = j < sum_blocks;
-            int pos;
-            const int row = j < j1 ? cache_row(j, pos) : 0;
+            const int row = sum ? j * T::KEYS : slot;
+            if (!sum && j < j1) slot = slot + T::KEYS == c.R ? 0 : slot + T::KEYS;
             const size_t at = bg * (size_t)(sum ? c.S_max : c.R) + row;
             const unsigned bytes = j < j1 ? T::KEYS * T::ROWB : 0;  // past the last: zeros, no access
             uintptr_t k, v;
@@ -178,19 +188,9 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(TreeParams a) {
         for (int i = 0; i < NS - 1; ++i) request(j0 + i, i);
     }
 
-    // ---- the wave's columns ----
-    const int col0 = (cb * WC + wc) * 32;
-    const int col = min(col0 + c32, a.cols - 1);  // past the last: the last again, not stored
     unsigned long long line;
     int lo, n_sum;
     rows.node(a, col % a.fT, line, lo, n_sum);
-    bf16x8 qf[NDC];  // features 16 dc + 8 h2 ..; 8-bit: step 2p + e has 32 p + 16 h2 + 8 e ..
-    {
-        const bf16* q = static_cast<const bf16*>(a.q) + (bg * a.cols + col) * D;
-#pragma unroll
-        for (int dc = 0; dc < NDC; ++dc)
-            qf[dc] = *reinterpret_cast<const bf16x8*>(q + (Q8 ? 32 * (dc >> 1) + 16 * h2 + 8 * (dc & 1) : 16 * dc + 8 * h2));
-    }
     floatx16 acc[NDB];
 #pragma unroll
     for (int db = 0; db < NDB; ++db) acc[db] = floatx16{};
@@ -223,8 +223,7 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(TreeParams a) {
     auto cache_block = [&](int j, const unsigned char* st) {
         const unsigned char *ks = st, *vs = st + Stage::BLK;
         const bool is_sum = j < sum_blocks;
-        int pos0;
-        cache_row(j, pos0);
+        const int pos0 = (is_sum ? j : win0 + j - sum_blocks) * T::KEYS;
         int key_lo = 0, key_hi;  // keys that some column sees
         bool full;               // every column sees every key
         if (is_sum) {
