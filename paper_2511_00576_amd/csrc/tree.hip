@@ -415,6 +415,7 @@ __global__ __launch_bounds__(NW * 64) void tree_f32_kernel(TreeParams a) {
         qf[j] = *reinterpret_cast<const floatx4*>(qrow + 16 * j + 4 * g);
         acc[j] = floatx4{0.f, 0.f, 0.f, 0.f};
     }
+    uint32_t special[D / 64] = {};  // not_finite_outputs, four feature blocks each
     float m_run = -INFINITY, l_run = 0.f;
 
     const int sum_chunks = (sum_last + 31) / 32;
@@ -447,25 +448,38 @@ __global__ __launch_bounds__(NW * 64) void tree_f32_kernel(TreeParams a) {
             key_hi = min(31, n - 1 - pos0);
             full = pos0 >= lo_last && key_hi == 31;
         }
-        const unsigned span = (unsigned)(key_hi - key_lo);
         // keys of this lane's column: first .. last, or its line
         const int first = draft || is_sum ? 0 : max(lo - pos0, key_lo);
         const int last = is_sum ? min(n_sum - pos0 - 1, key_hi) : key_hi;
         const uint32_t seen = draft ? (uint32_t)(line >> pos0) : 0xffffffffu;
-        floatx4 s[2];
-        float pw[2][4];
+        // all keys of the chunk before any wait (a drafted row past the last node:
+        // the last one's), all values before the softmax
+        floatx4 kf[2][NJ];
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
-            s[kb] = floatx4{0.f, 0.f, 0.f, 0.f};
-            // a drafted row past the last node is not there: the last one's
-            const int key = draft ? min(16 * kb + c16, key_hi) : 16 * kb + c16;
-            const float* krow = kt + (size_t)key * D + 4 * g;
+            const float* krow = kt + (size_t)(draft ? min(16 * kb + c16, key_hi) : 16 * kb + c16) * D + 4 * g;
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) {
-                const floatx4 kf = *reinterpret_cast<const floatx4*>(krow + 16 * j);
+            for (int j = 0; j < NJ; ++j) kf[kb][j] = *reinterpret_cast<const floatx4*>(krow + 16 * j);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        floatx4 s[2];
+        float pw[2][4];
+        // (four sums in turn: a product waits for the one before on the same sum)
+        floatx4 s2[2];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[kb] = mfma_f32(kf[e], qf[j][e], s[kb]);
-            }
+        for (int kb = 0; kb < 2; ++kb) s[kb] = s2[kb] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; e += 2)
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb) {
+                    s[kb] = mfma_f32(kf[kb][j][e], qf[j][e], s[kb]);
+                    s2[kb] = mfma_f32(kf[kb][j][e + 1], qf[j][e + 1], s2[kb]);
+                }
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            s[kb] += s2[kb];
             if (!full) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -474,6 +488,22 @@ __global__ __launch_bounds__(NW * 64) void tree_f32_kernel(TreeParams a) {
                 }
             }
         }
+        floatx4 vf[2][NJ];
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            const float* vtile = vt + (size_t)(2 * kb + (g >> 1)) * (kVtTile * D) + 4 * (g & 1);
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+                if (draft) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        vf[kb][j][i] = vt[(size_t)min(16 * kb + 4 * g + i, key_hi) * D + 16 * j + c16];
+                } else {
+                    vf[kb][j] = *reinterpret_cast<const floatx4*>(vtile + (16 * j + c16) * kVtTile);
+                }
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
         const float bias = is_sum ? a.log2C : 0.f;
         float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
                          fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
@@ -495,51 +525,34 @@ __global__ __launch_bounds__(NW * 64) void tree_f32_kernel(TreeParams a) {
             }
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
-            const float* vtile = vt + (size_t)(2 * kb + (g >> 1)) * (kVtTile * D) + 4 * (g & 1);
+            if (!full) {
+                // stale slots (no weight, whatever bits they hold), and values that
+                // some columns do not see: see not_finite_outputs
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) {
-                floatx4 vf;
-                if (draft) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        vf[i] = vt[(size_t)min(16 * kb + 4 * g + i, key_hi) * D + 16 * j + c16];
-                } else {
-                    vf = *reinterpret_cast<const floatx4*>(vtile + (16 * j + c16) * kVtTile);
-                }
-                if (!full) {
+                for (int j = 0; j < NJ; ++j) {
+                    floatx4& v = vf[kb][j];
                     bool bad = false;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const unsigned rel = (unsigned)(16 * kb + 4 * g + i - key_lo);
-                        vf[i] = rel <= span ? vf[i] : 0.f;
-                        bad |= !is_finite(vf[i]);
-                    }
+                    for (int i = 0; i < 4; ++i) bad |= !is_finite(v[i]);
                     if (__builtin_amdgcn_ballot_w64(bad)) {
-                        // a weight of 0 times it would be NaN: finite values as
-                        // they are, of the others what their weights make of them
-                        const floatx4 zero{0.f, 0.f, 0.f, 0.f};
-                        floatx4 cn = zero, ci = zero, cm = zero;
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            const float x = vf[i];
-                            cn = mfma_f32(x != x ? 1.f : 0.f, pw[kb][i], cn);
-                            ci = mfma_f32(x == INFINITY ? 1.f : 0.f, pw[kb][i], ci);
-                            cm = mfma_f32(x == -INFINITY ? 1.f : 0.f, pw[kb][i], cm);
-                            vf[i] = is_finite(x) ? x : 0.f;
-                        }
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            if (cn[i] > 0.f) acc[j][i] = NAN;
-                            if (ci[i] > 0.f) acc[j][i] += INFINITY;
-                            if (cm[i] > 0.f) acc[j][i] -= INFINITY;
+                            special[j / 4] |= not_finite_outputs_f32(v[i], pw[kb][i]) << (8 * (j % 4));
+                            v[i] = is_finite(v[i]) ? v[i] : 0.f;
                         }
                     }
                 }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) acc[j] = mfma_f32(vf[i], pw[kb][i], acc[j]);
             }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) acc[j] = mfma_f32(vf[kb][j][i], pw[kb][i], acc[j]);
         }
     }
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[j][i] = with_not_finite(acc[j][i], special[j / 4] >> (8 * (j % 4) + 2 * i) & 3);
 
     // ---- join the waves ----
     float* red_m = tree_smem;

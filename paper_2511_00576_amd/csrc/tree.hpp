@@ -132,6 +132,23 @@ __device__ __forceinline__ uint32_t not_finite_outputs(const bf16x8& v, const bf
     }
     return bits;
 }
+// The same of one step of four fp32 keys (16x16x4): v is the lane's feature of its
+// group's key, p its column's weight on it.
+__device__ __forceinline__ uint32_t not_finite_outputs_f32(float v, float p) {
+    const int lane = lane_here(), col = lane % 16, g = lane / 16;
+    uint32_t bits = 0;
+#pragma unroll 1
+    for (int from = 0; from < 64; from += 16) {
+        const float pk = __shfl(p, from + col, 64);
+#pragma unroll 1
+        for (int i = 0; i < 4; ++i) {
+            const float x = __shfl(v, from + 4 * g + i, 64);
+            const uint32_t kind = x != x ? 3 : x == INFINITY ? 1 : x == -INFINITY ? 2 : 0;
+            if (pk != 0.f) bits |= kind << (2 * i);
+        }
+    }
+    return bits;
+}
 __device__ __forceinline__ float with_not_finite(float o, uint32_t kind) {
     return kind == 0 ? o : kind == 1 ? o + INFINITY : kind == 2 ? o - INFINITY : NAN;
 }
