@@ -35,6 +35,9 @@ struct CacheTile {
     static constexpr int GRP = 1024 + (Q8 ? 32 : 64);
     static constexpr int GROUPS = KEYS * ROWB / 1024;
     static constexpr int NI = GROUPS / 4;  // requests per wave
+    // A bf16 ring and its summaries are a multiple of 32 rows: of a block of 64 each
+    // half has its own place.  (An 8-bit cache's are a multiple of 64.)
+    static constexpr int PARTS = !Q8 && KEYS == 64 ? 2 : 1;
     static constexpr int SUB = KEYS / 32 / (4 / WC);  // 32-key sub-blocks of a wave
     static __device__ __forceinline__ int row_at(int r) { return r / RPI * GRP + r % RPI * ROWB; }
     static __device__ __forceinline__ int swz(int r) { return (ROWB == 256 ? r : ROWB == 128 ? r >> 1 : r >> 2) & 3; }
@@ -55,6 +58,14 @@ struct WideStage {
     static constexpr int BYTES = 2 * BLK + EXP;
     static constexpr int NS = BYTES > 24 * 1024 ? 2 : 3;  // stages: two workgroups a CU at least
 };
+
+// Buffer descriptor of `bytes` bytes at p, wave-uniform also where the compiler
+// computed it in vector registers.
+__device__ __forceinline__ u32x4 scalar_desc(uintptr_t p, unsigned bytes) {
+    return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)p),
+                 (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(p >> 32)) & 0xffffu,
+                 (uint32_t)__builtin_amdgcn_readfirstlane(bytes), 0x00020000u};
+}
 
 // Two of a raw 16-byte read's contraction steps: the low or high eight codes.
 __device__ __forceinline__ bf16x8 half_codes(const u32x4& w, int e) { return q_bf16x8(w[2 * e], w[2 * e + 1]); }
@@ -134,10 +145,7 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(TreeParams a) {
         const unsigned base = lds0 + stage * Stage::BYTES;
         if (j < cache_blocks || j >= j1) {
             const bool sum = j < sum_blocks;
-            const int row = sum ? j * T::KEYS : slot;
-            if (!sum && j < j1) slot = slot + T::KEYS == c.R ? 0 : slot + T::KEYS;
-            const size_t at = bg * (size_t)(sum ? c.S_max : c.R) + row;
-            const unsigned bytes = j < j1 ? T::KEYS * T::ROWB : 0;  // past the last: zeros, no access
+            const size_t at = bg * (size_t)(sum ? c.S_max : c.R);  // the array's first row
             uintptr_t k, v;
             if constexpr (Q8) {
                 k = (uintptr_t)(sum ? a.qc.k_sum : a.qc.k_ring);
@@ -146,22 +154,30 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(TreeParams a) {
                 k = (uintptr_t)(sum ? c.k_sum : c.k_ring);
                 v = (uintptr_t)(sum ? c.vt_sum : c.vt_ring);
             }
-            k += at * T::ROWB;
-            v += at * T::ROWB;
-            const u32x4 dk{(uint32_t)k, (uint32_t)(k >> 32) & 0xffffu, bytes, 0x00020000u};
-            const u32x4 dv{(uint32_t)v, (uint32_t)(v >> 32) & 0xffffu, bytes, 0x00020000u};
+            int row = __builtin_amdgcn_readfirstlane(sum ? j * T::KEYS : slot);  // (descriptors lie in scalar registers)
 #pragma unroll
-            for (int i = 0; i < T::NI; ++i) dma16(dk, k_off, i * 4096, base + (4 * i + wave) * T::GRP);
+            for (int p = 0; p < T::PARTS; ++p) {
+                // past the last block, or the last summary there is room for: zeros,
+                // no access
+                const unsigned bytes = j < j1 && (!sum || row < c.S_max) ? T::KEYS / T::PARTS * T::ROWB : 0;
+                const u32x4 dk = scalar_desc(k + (at + row) * T::ROWB, bytes), dv = scalar_desc(v + (at + row) * T::ROWB, bytes);
+                constexpr int NP = T::NI / T::PARTS;
 #pragma unroll
-            for (int i = 0; i < T::NI; ++i) dma16(dv, v_off, i * 4096, base + Stage::BLK + (4 * i + wave) * T::GRP);
-            if constexpr (Q8) {
-                const uintptr_t ke = (uintptr_t)(sum ? a.qc.k_sum_e : a.qc.k_ring_e) + at;
-                const uintptr_t ve = (uintptr_t)(sum ? a.qc.v_sum_e : a.qc.v_ring_e) + at;
-                const unsigned eb = bytes ? 64 : 0;
-                const unsigned to = base + 2 * Stage::BLK + wave * 512;
-                dma4(u32x4{(uint32_t)ke, (uint32_t)(ke >> 32) & 0xffffu, eb, 0x00020000u}, lane * 4, to);
-                dma4(u32x4{(uint32_t)ve, (uint32_t)(ve >> 32) & 0xffffu, eb, 0x00020000u}, lane * 4, to + 256);
+                for (int i = 0; i < NP; ++i) {
+                    const unsigned to = base + (4 * (p * NP + i) + wave) * T::GRP;
+                    dma16(dk, k_off, i * 4096, to);
+                    dma16(dv, v_off, i * 4096, to + Stage::BLK);
+                }
+                if constexpr (Q8) {
+                    const unsigned to = base + 2 * Stage::BLK + wave * 512;
+                    dma4(scalar_desc((uintptr_t)(sum ? a.qc.k_sum_e : a.qc.k_ring_e) + at + row, bytes ? 64 : 0), lane * 4, to);
+                    dma4(scalar_desc((uintptr_t)(sum ? a.qc.v_sum_e : a.qc.v_ring_e) + at + row, bytes ? 64 : 0), lane * 4,
+                         to + 256);
+                }
+                row += T::KEYS / T::PARTS;
+                if (!sum && row == c.R) row = 0;
             }
+            if (!sum && j < j1) slot = row;
         } else {
             const int k0 = (j - cache_blocks) * 32;
             const size_t at = (bg * (size_t)a.T + k0) * DT::ROWB;

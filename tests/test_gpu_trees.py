@@ -99,6 +99,29 @@ def test_tree(kind, shape):
     run(kind, B, H, Hkv, d, W, C, lens, T, window, seed=T + W)
 
 
+# more than 512 workgroups of 16 columns: the shapes that bf16 and 8-bit caches
+# take through LDS, 64 columns a workgroup or 128
+WIDE = [
+    (66, 8, 2, 128, 64, 16, 13, SLIDING),   # 52 columns
+    (129, 4, 2, 64, 20, 5, 20, ALIGNED),    # 40, T = W
+    (18, 16, 2, 64, 100, 33, 63, SLIDING),  # 504
+    (17, 8, 1, 128, 64, 8, 64, SLIDING),    # 512, the largest tree
+    (40, 24, 2, 128, 33, 7, 12, ALIGNED),   # 144
+]
+
+
+def wide_lens(B):
+    return [(37 * i) % 200 if i % 5 else 300 + i for i in range(B)]
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3", "f32"])
+@pytest.mark.parametrize("shape", WIDE)
+def test_many_columns(kind, shape):
+    B, H, Hkv, d, W, C, T, window = shape
+    assert B * Hkv * -(-H // Hkv * T // 16) > 512
+    run(kind, B, H, Hkv, d, W, C, wide_lens(B), T, window, seed=T + W)
+
+
 @pytest.mark.parametrize("kind", ["bf16", "e4m3", "f32"])
 @pytest.mark.parametrize("T", [2, 20])
 def test_long_rows_are_split_and_joined(kind, T):
@@ -118,12 +141,13 @@ def test_many_units(kind):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "e4m3", "f32"])
-def test_sizes_activity_and_rows_left_as_they_were(kind):
-    B, H, Hkv, d, W, C, T = 5, 8, 2, 128, 64, 16, 20
-    cache, models, dtype = start(kind, B, H, Hkv, d, W, C, [100, 3, 0, 64, 200], SLIDING, 3)
+@pytest.mark.parametrize("times", [1, 12])  # 12: shapes of many columns
+def test_sizes_activity_and_rows_left_as_they_were(kind, times):
+    B, H, Hkv, d, W, C, T = 5 * times, 8, 2, 128, 64, 16, 20
+    cache, models, dtype = start(kind, B, H, Hkv, d, W, C, [100, 3, 0, 64, 200] * times, SLIDING, 3)
     q, k, v = draft(B, H, Hkv, T, d, dtype, 3)
     parents = random_tree(B, T, torch.Generator().manual_seed(4))
-    nodes, active = [20, 7, 1, 0, 13], [1, 1, 1, 1, 0]
+    nodes, active = [20, 7, 1, 0, 13] * times, [1, 1, 1, 1, 0] * times
     # absent nodes hold what a padded batch may hold
     for b in range(B):
         parents[b, nodes[b]:] = 10 ** 9
@@ -141,7 +165,7 @@ def test_sizes_activity_and_rows_left_as_they_were(kind):
     # sizes out of range are clamped
     o = eva.tree_attention(cache, q[:, :, :5].contiguous().cuda(), k[:, :, :5].contiguous().cuda(),
                            v[:, :, :5].contiguous().cuda(), parents[:, :5].contiguous().cuda(),
-                           n_nodes=torch.tensor([9, 5, -3, 0, 5], dtype=torch.int32, device="cuda"),
+                           n_nodes=torch.tensor([9, 5, -3, 0, 5] * times, dtype=torch.int32, device="cuda"),
                            out=torch.full((B, H, 5, d), 7.0, dtype=dtype, device="cuda"))
     check(o[:2], q[:2, :, :5], k[:2, :, :5], v[:2, :, :5], parents[:2], models[:2], dtype)
     assert (o[2:4] == 7).all()
@@ -159,15 +183,16 @@ def test_parents_that_name_no_earlier_node_make_roots(kind):
 
 @pytest.mark.parametrize("kind", ["bf16", "e4m3", "f32"])
 @pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
-def test_values_that_are_not_finite_reach_only_the_rows_that_see_them(kind, bad):
+@pytest.mark.parametrize("B,H", [(1, 4), (172, 4), (90, 8)])  # 16, 64 and 128 columns a workgroup
+def test_values_that_are_not_finite_reach_only_the_rows_that_see_them(kind, bad, B, H):
     """A drafted sibling, a position that only shallow nodes still see, and the
     newest summary that only deep ones see."""
-    B, H, Hkv, d, W, C, T, n = 1, 4, 1, 64, 32, 8, 12, 103
+    Hkv, d, W, C, T, n = 1, 64, 32, 8, 12, 103
     dtype = F32 if kind == "f32" else BF16
-    parents = torch.tensor([[-1, 0, 1, 2, 3, 4, 5, 6, 7, 0, 9, -1]], dtype=torch.int32)
+    parents = torch.tensor([[-1, 0, 1, 2, 3, 4, 5, 6, 7, 0, 9, -1]] * B, dtype=torch.int32)
     depth = [len(line_of(parents[0].tolist(), t)) - 1 for t in range(T)]
-    q, k, v = draft(B, H, Hkv, T, d, dtype, 8)
-    _, K, V = inputs.qkv(B, H, Hkv, n, d, dtype, seed=8)
+    q, k, v = (x.repeat(B, 1, 1, 1) for x in draft(1, H, Hkv, T, d, dtype, 8))
+    _, K, V = (x.repeat(B, 1, 1, 1) for x in inputs.qkv(1, H, Hkv, n, d, dtype, seed=8))
     Ks, Vs = (t.cpu() for t in eva.build_summaries(K.cuda(), V.cuda(), C))
     lo = [first for first in (n + dd - W + 1 for dd in depth)]
     place = n - W + 3          # seen up to depth 2
@@ -175,22 +200,23 @@ def test_values_that_are_not_finite_reach_only_the_rows_that_see_them(kind, bad)
     for what in ("draft", "ring", "summary"):
         k2, v2, V2, Vs2 = k.clone(), v.clone(), V.clone(), Vs.clone()
         if what == "draft":
-            v2[0, 0, 9, 5] = bad   # node 9: seen by 9 and 10
+            v2[:, 0, 9, 5] = bad   # node 9: seen by 9 and 10
             sees = [9 in line_of(parents[0].tolist(), t) for t in range(T)]
         elif what == "ring":
-            V2[0, 0, place, 5] = bad
+            V2[:, 0, place, 5] = bad
             sees = [x <= place for x in lo]
         else:
-            Vs2[0, 0, chunk, 5] = bad
+            Vs2[:, 0, chunk, 5] = bad
             sees = [x // C > chunk for x in lo]
         assert any(sees) and not all(sees)
         if kind == "e4m3":
             cache = eva.QuantCache(B, H, Hkv, d, W, C, max_tokens=n + 64, fill=math.nan)
-            eva.qcache_fill(cache, K.cuda(), V2.cuda(), Ks.cuda(), Vs2.cuda(), torch.tensor([n], dtype=torch.int32, device="cuda"))
+            eva.qcache_fill(cache, K.cuda(), V2.cuda(), Ks.cuda(), Vs2.cuda(), torch.tensor([n] * B, dtype=torch.int32, device="cuda"))
         else:
             cache = eva.RaggedCache(B, H, Hkv, d, W, C, max_tokens=n + 64, dtype=dtype, fill=math.nan)
-            eva.rcache_fill(cache, K.cuda(), V2.cuda(), Ks.cuda(), Vs2.cuda(), torch.tensor([n], dtype=torch.int32, device="cuda"))
+            eva.rcache_fill(cache, K.cuda(), V2.cuda(), Ks.cuda(), Vs2.cuda(), torch.tensor([n] * B, dtype=torch.int32, device="cuda"))
         o = eva.tree_attention(cache, q.cuda(), k2.cuda(), v2.cuda(), parents.cuda()).cpu().float()
+        assert torch.equal(o.isnan(), o[:1].expand_as(o).isnan()) and torch.equal(o.nan_to_num(), o[:1].expand_as(o).nan_to_num())
         # an 8-bit row holds NaN for what is not finite
         want = math.nan if kind == "e4m3" and what != "draft" else bad
         for t in range(T):
