@@ -985,19 +985,34 @@ int row_chunks(int window, int max_tok, int W, int C, int S_max, int keys) {
 }
 
 // How the query columns of a kv head and its keys are laid over workgroups: what
-// a launch does and what the workspace queries answer.
+// a launch does and what the workspace queries answer.  Times on MI355X in a
+// captured graph, us, d = 128, W = 512, 60 summaries (8-bit: 11 chunks, bf16: 21).
+//
+// Blocks of 16 columns, which read the rows again each, or of 64 or 128 through
+// LDS: 16 as long as their workgroups are two a CU at most (units x columns, 16 /
+// 64 or 128: e4m3 8 x 256 12.2 / 19.9, 64 x 128 17.7 / 29.1, 128 x 64 17.4 / 27.2;
+// bf16 8 x 256 15.4 / 17.0, 64 x 128 18.7 / 26.1, 128 x 64 18.7 / 24.2) or two
+// blocks hold them all (512 x 32: e4m3 31.0 / 30.3, bf16 43.0 / 38.9, but 256 x 32:
+// 17.7 / 24.5 and 19.4 / 22.4), else the wider (512 x 48: e4m3 38.2 / 31.9, bf16
+// 51.5 / 39.2; 256 x 256: bf16 123 / 38).  Of those 64 columns a workgroup up to
+// 64 (512 x 48 e4m3: 36 with 64, 51 with 128), else 128 (256 x 256 bf16: 58 / 46).
+//
+// 16 columns: 12 waves a workgroup instead of 4 while every workgroup has a CU and
+// few rounds of chunks (8-bit decode, 12 waves / 4, split where there are few
+// units: 8 x 10 8.1 / 10.0 with the join, 128 x 10 9.7 / 12.6, 256 x 10 11.1 / 12.8;
+// 8 x 20 11.2 / 9.8).
 struct TreeRoute {
     int shape, col_blocks, splits;
     size_t ws_bytes;
 };
 TreeRoute tree_route(long long units, long long cols, int d, int dtype, bool drafted, int n_chunks) {
     TreeRoute r;
-    const bool wide = dtype == EVA_BF16 && drafted && cols > 32;
+    const bool wide = dtype == EVA_BF16 && drafted && cols > 32 && units * ((cols + 15) / 16) > 512;
     r.shape = !wide ? eva::kTreeNarrow : cols <= 64 ? eva::kTree64 : eva::kTree128;
     const int per = !wide ? 16 : cols <= 64 ? 64 : 128;
     const long long blocks = (cols + per - 1) / per, wgs = units * blocks;
     r.col_blocks = (int)blocks;
-    if (!wide && wgs < 256 && n_chunks > 4 && n_chunks <= 20) r.shape = eva::kTreeNarrow12;
+    if (!wide && wgs <= 256 && n_chunks > 4 && n_chunks <= 20) r.shape = eva::kTreeNarrow12;
     r.splits = 1;
     if (r.shape != eva::kTreeNarrow12 && wgs < 256) {
         long long s = (512 + wgs - 1) / wgs;
