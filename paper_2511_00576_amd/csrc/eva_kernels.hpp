@@ -270,6 +270,7 @@ struct NormRopeParams {
     void* V;
     int H, Hkv, tokens;  // tokens = B L
     FastDiv fL;          // divisor of L
+    int pack;            // the launch's: a wave holds 1 << pack tokens
     // backward
     const void* dQ;
     const void* dK;
@@ -280,15 +281,15 @@ struct NormRopeParams {
     float* ws;   // [workgroups][2][d]: shares of dgq and dgk
 };
 template <int D, typename T>
-hipError_t launch_norm_rope(const NormRopeParams& p, hipStream_t stream);
+hipError_t launch_norm_rope(NormRopeParams p, hipStream_t stream);
 // Workgroups of the backward: a wave per token, up to the three workgroups a CU
 // holds at once (B4 L4096 H32/8 d128: 120 us with 768, 145 with 1024).
-inline int norm_rope_bwd_wgs(int tokens) {
+inline int norm_rope_bwd_wgs(int tokens) {  // (or groups of tokens that share a wave)
     const int n = (tokens + 3) / 4;
     return n < 768 ? n : 768;
 }
 template <int D, typename T>
-hipError_t launch_norm_rope_backward(const NormRopeParams& p, hipStream_t stream);
+hipError_t launch_norm_rope_backward(NormRopeParams p, hipStream_t stream);
 
 // The 8-bit cache (qrows.hpp): codes and exponent bytes, per (b, kv head).
 struct QCacheView {

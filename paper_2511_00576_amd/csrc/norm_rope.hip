@@ -15,7 +15,8 @@
 // A row is held by D / 16 lanes of 16 features, as two 8-feature chunks that
 // hold both members of the lane's eight pairs, so a turn stays in the lane;
 // a wave works on 1024 / D rows of one token at a time and computes the
-// token's angles once for all its heads.  Angles are whole numbers: p times
+// token's angles once for all its heads.  Where the queries' heads would leave
+// half of the lanes idle or more, a wave holds several tokens.  Angles are whole numbers: p times
 // the frequency in 2^-64 turns, modulo 2^64, is exact to 2^-64 p turns at any
 // position, where a product in fp32 is off by radians from 2^24 on.
 #include "eva_device.hpp"
@@ -73,18 +74,26 @@ __device__ __forceinline__ void store8(float* p, const float x[8]) {
 }
 
 // Where a lane's two chunks lie and how its pairs are formed.
-// ADJ: pairs are adjacent features.
-template <int D, bool ADJ>
+// ADJ: pairs are adjacent features.  PACK: a wave holds 1 << a.pack tokens, each
+// with all its heads of a kind in one sweep; else one token.
+template <int D, bool ADJ, bool PACK>
 struct LaneRow {
     static constexpr int kLanes = D / 16;           // lanes per row
     static constexpr int kRows = 64 / kLanes;       // rows per wave
     int c, sub;                                     // place in the row, row in the wave
+    int h, t;                                       // its head in a sweep, its token in the wave
     int f0, f1;                                     // first feature of the chunks
     bool turned;                                    // its pairs are turned
     __device__ LaneRow(const NormRopeParams& a) {
         const int lane = threadIdx.x & 63;
         c = lane % kLanes;
         sub = lane / kLanes;
+        h = sub;
+        t = 0;
+        if constexpr (PACK) {
+            h = sub & ((kRows >> a.pack) - 1);
+            t = sub / (kRows >> a.pack);
+        }
         turned = 16 * c < a.rot;
         // halves: pair i is (i, i + rot / 2), so chunk c goes with chunk c + rot / 16;
         // the features that are not turned, and adjacent pairs, lie side by side
@@ -137,8 +146,8 @@ __device__ __forceinline__ void cos_sin(unsigned long long t, float& c, float& s
 }
 
 // cos and sin of the lane's eight pairs at a token's position.
-template <int D, bool ADJ>
-__device__ __forceinline__ void angles(const NormRopeParams& a, const LaneRow<D, ADJ>& r, int tok, float (&cs)[8], float (&sn)[8]) {
+template <typename Row>
+__device__ __forceinline__ void angles(const NormRopeParams& a, const Row& r, int tok, float (&cs)[8], float (&sn)[8]) {
     if (!r.turned) return;
     const int b = tok / a.fL, l = tok - b * a.fL.d;
     const long long pos = (long long)(a.start ? a.start[b] : 0) + (a.offsets ? a.offsets[tok] : l);
@@ -157,12 +166,14 @@ struct Sweeps {
     }
 };
 
-// One wave per token (and part of its heads where there are few tokens).
-template <int D, typename T, bool ADJ>
+// One wave per token (and part of its heads where there are few tokens), or per
+// 1 << a.pack tokens.
+template <int D, typename T, bool ADJ, bool PACK>
 __global__ __launch_bounds__(kNormRopeWaves * 64) void norm_rope_kernel(NormRopeParams a) {
-    const LaneRow<D, ADJ> r(a);
-    const int tok = blockIdx.x * kNormRopeWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (tok >= a.tokens) return;
+    const LaneRow<D, ADJ, PACK> r(a);
+    int tok = blockIdx.x * kNormRopeWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if constexpr (PACK) tok = (tok << a.pack) + r.t;
+    if (tok >= a.tokens) return;  // (all lanes of a row together)
     const int b = tok / a.fL, l = tok - b * a.fL.d;
     const Sweeps sw(a, r.kRows);
     const T* xt = static_cast<const T*>(a.x) + b * a.stride_b + l * a.stride_l;
@@ -173,7 +184,7 @@ __global__ __launch_bounds__(kNormRopeWaves * 64) void norm_rope_kernel(NormRope
     auto sweep = [&](int s) {
         const int kind = s < sw.q ? 0 : s < sw.k ? 1 : 2;
         return Sweep{kind, kind == 0 ? 0 : kind == 1 ? a.H : a.H + a.Hkv, kind == 0 ? a.H : a.Hkv,
-                     (s - (kind == 0 ? 0 : kind == 1 ? sw.q : sw.k)) * r.kRows + r.sub};
+                     (s - (kind == 0 ? 0 : kind == 1 ? sw.q : sw.k)) * r.kRows + r.h};
     };
     RawRow<T> raw;
     auto request = [&](const Sweep& w) { raw.load(xt + (size_t)(w.first + min(w.h, w.heads - 1)) * D, r.f0, r.f1); };
@@ -212,20 +223,21 @@ __global__ __launch_bounds__(kNormRopeWaves * 64) void norm_rope_kernel(NormRope
 // gradients stays in registers, its workgroup's sum goes to its own place of
 // the workspace, and a second launch adds those up in their order: the same
 // bits every time.
-template <int D, typename T, bool ADJ>
+template <int D, typename T, bool ADJ, bool PACK>
 __global__ __launch_bounds__(kNormRopeWaves * 64, 3) void norm_rope_bwd_kernel(NormRopeParams a) {
-    const LaneRow<D, ADJ> r(a);
+    const LaneRow<D, ADJ, PACK> r(a);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Sweeps sw(a, r.kRows);
     float dg[2][16] = {};
-    for (int tok = blockIdx.x * kNormRopeWaves + wave; tok < a.tokens; tok += gridDim.x * kNormRopeWaves) {
+    const int pack = PACK ? a.pack : 0;
+    for (int tok = ((blockIdx.x * kNormRopeWaves + wave) << pack) + r.t; tok < a.tokens; tok += gridDim.x * kNormRopeWaves << pack) {
         const int b = tok / a.fL, l = tok - b * a.fL.d;
         const T* xt = static_cast<const T*>(a.x) + b * a.stride_b + l * a.stride_l;
         T* dxt = static_cast<T*>(a.dx) + (size_t)tok * (a.H + 2 * a.Hkv) * D;
         float cs[8], sn[8];
         angles(a, r, tok, cs, sn);
         auto rows = [&](int s, int heads, int head0, const void* grad, const void* weight, float (&acc)[16]) {
-            const int h = s * r.kRows + r.sub;
+            const int h = s * r.kRows + r.h;
             const bool on = h < heads;
             const size_t row = (size_t)(head0 + min(h, heads - 1)) * D;
             float dy[16];
@@ -255,7 +267,7 @@ __global__ __launch_bounds__(kNormRopeWaves * 64, 3) void norm_rope_bwd_kernel(N
         for (int s = 0; s < sw.q; ++s) rows(s, a.H, 0, a.dQ, a.gq, dg[0]);
         for (int s = sw.q; s < sw.k; ++s) rows(s - sw.q, a.Hkv, a.H, a.dK, a.gk, dg[1]);
         for (int s = sw.k; s < sw.all; ++s) {
-            const int h = (s - sw.k) * r.kRows + r.sub;
+            const int h = (s - sw.k) * r.kRows + r.h;
             if (h >= a.Hkv) continue;
             float y[16];
             r.load(static_cast<const T*>(a.dV) + (((size_t)b * a.Hkv + h) * a.fL.d + l) * D, y);
@@ -313,30 +325,43 @@ __global__ __launch_bounds__(1024) void norm_rope_sum_kernel(const float* __rest
 
 }  // namespace
 
+// log2 of the tokens a wave holds: as many as fit with all their query heads.
+// (us a launch on MI355X, several tokens a wave / one: bf16 d64 H1 B28 L1300 8.6 /
+// 36.5 and backward 14.7 / 44.8, d128 H4/1 B16 L1300 17.1 / 23.8 and 28 / 44, fp32
+// d64 H8/2 B16 L1300 32.0 / 36.5 and 42.7 / 67.)
+template <int D>
+int tokens_log2(int H) {
+    int n = 0;
+    while (H << (n + 1) <= 1024 / D) ++n;
+    return n;
+}
+
 template <int D, typename T>
-hipError_t launch_norm_rope(const NormRopeParams& p, hipStream_t stream) {
+hipError_t launch_norm_rope(NormRopeParams p, hipStream_t stream) {
     constexpr int rows = 1024 / D;
+    p.pack = tokens_log2<D>(p.H);
     const int sweeps = (p.H + rows - 1) / rows + 2 * ((p.Hkv + rows - 1) / rows);
-    const int wgs = (p.tokens + kNormRopeWaves - 1) / kNormRopeWaves;
+    const int per = kNormRopeWaves << p.pack, wgs = (p.tokens + per - 1) / per;
     // few tokens: their heads over workgroups, until there are four waves a CU
     int split = (256 + wgs - 1) / wgs;
     if (split > sweeps) split = sweeps;
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(wgs, split), dim3(kNormRopeWaves * 64), 0, stream, p); };
     if (p.interleaved)
-        go(norm_rope_kernel<D, T, true>);
+        p.pack ? go(norm_rope_kernel<D, T, true, true>) : go(norm_rope_kernel<D, T, true, false>);
     else
-        go(norm_rope_kernel<D, T, false>);
+        p.pack ? go(norm_rope_kernel<D, T, false, true>) : go(norm_rope_kernel<D, T, false, false>);
     return hipGetLastError();
 }
 
 template <int D, typename T>
-hipError_t launch_norm_rope_backward(const NormRopeParams& p, hipStream_t stream) {
-    const int wgs = norm_rope_bwd_wgs(p.tokens);
+hipError_t launch_norm_rope_backward(NormRopeParams p, hipStream_t stream) {
+    p.pack = tokens_log2<D>(p.H);
+    const int wgs = norm_rope_bwd_wgs((p.tokens + (1 << p.pack) - 1) >> p.pack);
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(wgs), dim3(kNormRopeWaves * 64), 0, stream, p); };
     if (p.interleaved)
-        go(norm_rope_bwd_kernel<D, T, true>);
+        p.pack ? go(norm_rope_bwd_kernel<D, T, true, true>) : go(norm_rope_bwd_kernel<D, T, true, false>);
     else
-        go(norm_rope_bwd_kernel<D, T, false>);
+        p.pack ? go(norm_rope_bwd_kernel<D, T, false, true>) : go(norm_rope_bwd_kernel<D, T, false, false>);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || (!p.gq && !p.gk)) return e;
     hipLaunchKernelGGL((norm_rope_sum_kernel<D>), dim3(2 * D / kSumFeatures), dim3(1024), 0, stream, p.ws, wgs, p.dgq, p.dgk);
@@ -344,8 +369,8 @@ hipError_t launch_norm_rope_backward(const NormRopeParams& p, hipStream_t stream
 }
 
 #define EVA_NORM_ROPE(D, T)                                                             \
-    template hipError_t launch_norm_rope<D, T>(const NormRopeParams&, hipStream_t);     \
-    template hipError_t launch_norm_rope_backward<D, T>(const NormRopeParams&, hipStream_t);
+    template hipError_t launch_norm_rope<D, T>(NormRopeParams, hipStream_t);            \
+    template hipError_t launch_norm_rope_backward<D, T>(NormRopeParams, hipStream_t);
 EVA_NORM_ROPE(64, bf16)
 EVA_NORM_ROPE(128, bf16)
 EVA_NORM_ROPE(64, float)

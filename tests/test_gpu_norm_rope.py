@@ -125,6 +125,13 @@ CASES = [
     (2, 31, 5, 5, 64, 0, torch.float32, False, (True, True), 0, False),
     (2, 31, 4, 2, 64, 64, torch.bfloat16, False, (False, False), 9, False),
     (1, 4099, 17, 17, 128, 128, torch.float32, False, (True, True), 3, False),
+    # few heads: several tokens a wave, the last wave's part of the lanes idle
+    (3, 171, 1, 1, 128, 128, torch.bfloat16, True, (True, True), 50, True),
+    (5, 41, 2, 1, 64, 48, torch.float32, False, (True, True), 2 ** 20, False),
+    (2, 1, 3, 3, 64, 64, torch.bfloat16, False, (True, False), 0, False),
+    (7, 3000, 1, 1, 64, 32, torch.bfloat16, False, (True, True), 0, False),
+    (1, 17, 3, 1, 128, 16, torch.float32, True, (False, True), 9, False),
+    (2, 333, 8, 8, 64, 64, torch.bfloat16, True, (True, True), 0, False),
 ]
 
 
