@@ -997,10 +997,14 @@ int row_chunks(int window, int max_tok, int W, int C, int S_max, int keys) {
 // 51.5 / 39.2; 256 x 256: bf16 123 / 38).  Of those 64 columns a workgroup up to
 // 64 (512 x 48 e4m3: 36 with 64, 51 with 128), else 128 (256 x 256 bf16: 58 / 46).
 //
-// 16 columns: 12 waves a workgroup instead of 4 while every workgroup has a CU and
-// few rounds of chunks (8-bit decode, 12 waves / 4, split where there are few
-// units: 8 x 10 8.1 / 10.0 with the join, 128 x 10 9.7 / 12.6, 256 x 10 11.1 / 12.8;
-// 8 x 20 11.2 / 9.8).
+// 16 columns: 12 waves a workgroup instead of 4 while every workgroup has a CU, for
+// one round of chunks, or two where splits would bring few more CUs (12 waves / 4,
+// split where there are few units: 8-bit decode of 10 chunks, 8 units 8.1 / 10.0
+// with the join, 128 9.7 / 12.6, 256 11.1 / 12.8; trees of 20 chunks, 2 units 14.2 /
+// 11.2, 128 17.6 / 17.3, 240 18.8 / 22.8, bf16 11.3 / 9.2, 16.9 / 16.0, 17.9 / 22.0;
+// 35 chunks, 136 units 27.3 / 25.1).  fp32 products are slow enough to bound a CU of
+// 12 waves: only for one round and where splits bring few CUs (11 chunks, 2 units
+// 19.0 / 10.9, 128 22.4 / 18.8, 240 27.3 / 30.4; 19 chunks, 240 units 45.5 / 43.0).
 struct TreeRoute {
     int shape, col_blocks, splits;
     size_t ws_bytes;
@@ -1012,12 +1016,13 @@ TreeRoute tree_route(long long units, long long cols, int d, int dtype, bool dra
     const int per = !wide ? 16 : cols <= 64 ? 64 : 128;
     const long long blocks = (cols + per - 1) / per, wgs = units * blocks;
     r.col_blocks = (int)blocks;
-    if (!wide && wgs <= 256 && n_chunks > 4 && n_chunks <= 20) r.shape = eva::kTreeNarrow12;
+    const int most = dtype == EVA_F32 ? (wgs > 128 ? 12 : 0) : wgs > 128 ? 20 : 12;
+    if (!wide && wgs <= 256 && n_chunks > 4 && n_chunks <= most) r.shape = eva::kTreeNarrow12;
     r.splits = 1;
     if (r.shape != eva::kTreeNarrow12 && wgs < 256) {
         long long s = (512 + wgs - 1) / wgs;
-        const long long most = (n_chunks + 3) / 4;
-        r.splits = (int)(s > most ? most : s);
+        const long long rounds = (n_chunks + 3) / 4;
+        r.splits = (int)(s > rounds ? rounds : s);
     }
     r.ws_bytes = r.splits > 1 ? (size_t)units * r.splits * cols * (d + 2) * sizeof(float) : 0;
     return r;

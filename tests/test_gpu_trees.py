@@ -141,6 +141,13 @@ def test_many_units(kind):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "e4m3", "f32"])
+@pytest.mark.parametrize("d,T", [(64, 5), (128, 1)])
+def test_units_that_nearly_fill_the_chip(kind, d, T):
+    # 150 workgroups with a window of several chunks: not split, 12 waves each
+    run(kind, 50, 6, 3, d, 200, 16, wide_lens(50), T, SLIDING, seed=d + T)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3", "f32"])
 @pytest.mark.parametrize("times", [1, 12])  # 12: shapes of many columns
 def test_sizes_activity_and_rows_left_as_they_were(kind, times):
     B, H, Hkv, d, W, C, T = 5 * times, 8, 2, 128, 64, 16, 20
