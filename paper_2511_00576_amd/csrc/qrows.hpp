@@ -2,8 +2,7 @@
 // value = code 2^(byte - 127).  The exponent is the smallest whose power of
 // two brings the row's largest finite magnitude to 448, e4m3's largest value,
 // or below.  A power of two scales exactly both ways, so a code differs from
-// the row's value by its one rounding, the row's largest sum of squares has no
-// influence on it, and rows of the same values have the same codes wherever
+// the row's value by its one rounding, and rows of the same values have the same codes wherever
 // they are quantised; a row's small entries lose nothing either, since the
 // codes have exponents of their own (2^-6 and less of 448 becomes subnormal).
 #pragma once
@@ -76,6 +75,21 @@ __device__ __forceinline__ uint32_t q_bf16x2(uint32_t w) {
 // Eight codes as a matrix-core operand fragment.
 __device__ __forceinline__ bf16x8 q_bf16x8(uint32_t lo, uint32_t hi) {
     return __builtin_bit_cast(bf16x8, u32x4{q_bf16x2<false>(lo), q_bf16x2<true>(lo), q_bf16x2<false>(hi), q_bf16x2<true>(hi)});
+}
+
+// Whether one of 16 codes is a NaN.
+__device__ __forceinline__ bool q_has_nan(const u32x4& w) {
+    uint32_t x = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x |= (w[i] & 0x7f7f7f7fu) + 0x01010101u;  // bit 7 of a byte: it is 0x7f
+    return (x & 0x80808080u) != 0;
+}
+// 16 exponent bytes of which some may be stale: 255, an infinite scale, becomes
+// 254 (no row has it), so that a weight of zero stays zero.
+__device__ __forceinline__ u32x4 q_finite_scales(u32x4 w) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] ^= (((w[i] & 0x7f7f7f7fu) + 0x01010101u) & w[i] & 0x80808080u) >> 7;
+    return w;
 }
 
 // Eight bf16 features as fp32.

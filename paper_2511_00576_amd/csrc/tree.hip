@@ -295,16 +295,17 @@ __global__ __launch_bounds__(NW * 64, NW == 12 ? 3 : 2) void tree_kernel(TreePar
         }
         weights(s, bias);
         if constexpr (Q8) {
-            // (a stale slot's byte may be 255, an infinity: times no weight it stays none)
+            if (!full) vx = q_finite_scales(vx);
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) s[kb][i] = s[kb][i] == 0.f ? 0.f : s[kb][i] * q_scale(vx[kb] >> (8 * i) & 255);
+                for (int i = 0; i < 4; ++i) s[kb][i] *= q_scale(vx[kb] >> (8 * i) & 255);
             const bf16x8 p0 = pack8(s[0], s[1]), p1 = pack8(s[2], s[3]);  // keys 16g .., 16g + 8 ..
 #pragma unroll
             for (int db = 0; db < NDB; ++db) {
-                add(q_bf16x8(va[db][0], va[db][1]), p0, db, DRAFT && !full);
-                add(q_bf16x8(va[db][2], va[db][3]), p1, db, DRAFT && !full);
+                const bool nan = DRAFT && !full && __builtin_amdgcn_ballot_w64(q_has_nan(va[db]));
+                add(q_bf16x8(va[db][0], va[db][1]), p0, db, nan);
+                add(q_bf16x8(va[db][2], va[db][3]), p1, db, nan);
                 __builtin_amdgcn_sched_barrier(0);
             }
         } else {

@@ -293,6 +293,10 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(TreeParams a) {
                     const int key = 32 * sb + T::key_of(i, 0);
                     s[sb][i] = key >= first && key <= last ? s[sb][i] : -INFINITY;
                 }
+            if constexpr (Q8) {
+#pragma unroll
+                for (int sb = 0; sb < SUB; ++sb) vx[sb] = q_finite_scales(vx[sb]);
+            }
         }
         float mx = s[0][0];
 #pragma unroll
@@ -309,10 +313,9 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(TreeParams a) {
                 float p0 = fast_exp2(fmaf(s[sb][i], a.scale_log2, off)), p1 = fast_exp2(fmaf(s[sb][i + 1], a.scale_log2, off));
                 l_run += p0 + p1;
                 if constexpr (Q8) {
-                    // (a stale slot's byte may be 255, an infinity: times no weight it stays none)
                     const uint32_t x = vx[sb][i >> 2] >> (8 * (i & 3));
-                    p0 = p0 == 0.f ? 0.f : p0 * q_scale(x & 255);
-                    p1 = p1 == 0.f ? 0.f : p1 * q_scale(x >> 8 & 255);
+                    p0 *= q_scale(x & 255);
+                    p1 *= q_scale(x >> 8 & 255);
                 }
                 pf[sb][i >> 3][(i & 7) >> 1] = pack_bf16x2(p0, p1);
             }
@@ -329,8 +332,9 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(TreeParams a) {
                               [&](int k, const u32x4& w) {
                                   const int x = k / NDB;
                                   if constexpr (Q8) {
-                                      add(half_codes(w, 0), pf[x][0], k % NDB, !full);
-                                      add(half_codes(w, 1), pf[x][1], k % NDB, !full);
+                                      const bool nan = !full && __builtin_amdgcn_ballot_w64(q_has_nan(w));
+                                      add(half_codes(w, 0), pf[x][0], k % NDB, nan);
+                                      add(half_codes(w, 1), pf[x][1], k % NDB, nan);
                                   } else {
                                       add(__builtin_bit_cast(bf16x8, w), pf[0][x], k % NDB, !full);
                                   }

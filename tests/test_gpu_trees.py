@@ -140,6 +140,20 @@ def test_many_units(kind):
     run(kind, 75, 4, 4, 64, 40, 8, [(37 * i) % 200 for i in range(75)], 5, seed=9)
 
 
+@pytest.mark.parametrize("B,H,T", [(2, 4, 5), (130, 8, 10)])  # 16 and 64 columns a workgroup
+def test_stale_exponent_bytes(B, H, T):
+    """Bytes that no row has, where there is no row: of scales that are infinite."""
+    lens = [30 + 3 * (b % 7) for b in range(B)]
+    cache, models, dtype = start("e4m3", B, H, 2, 128, 100, 16, lens, SLIDING, 6)
+    q, k, v = draft(B, H, 2, T, 128, dtype, 6)
+    parents = random_tree(B, T, torch.Generator().manual_seed(6))
+    for b, n in enumerate(lens):
+        for ring, held in ((cache.k_ring_exp, n), (cache.v_ring_exp, n), (cache.k_sum_exp, n // 16), (cache.v_sum_exp, n // 16)):
+            ring[b, :, held:] = 255
+    o = eva.tree_attention(cache, q.cuda(), k.cuda(), v.cuda(), parents.cuda())
+    check(o, q, k, v, parents, models, dtype)
+
+
 @pytest.mark.parametrize("kind", ["bf16", "e4m3", "f32"])
 @pytest.mark.parametrize("d,T", [(64, 5), (128, 1)])
 def test_units_that_nearly_fill_the_chip(kind, d, T):
