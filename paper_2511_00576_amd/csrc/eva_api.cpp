@@ -1004,7 +1004,9 @@ int row_chunks(int window, int max_tok, int W, int C, int S_max, int keys) {
 // 11.2, 128 17.6 / 17.3, 240 18.8 / 22.8, bf16 11.3 / 9.2, 16.9 / 16.0, 17.9 / 22.0;
 // 35 chunks, 136 units 27.3 / 25.1).  fp32 products are slow enough to bound a CU of
 // 12 waves: only for one round and where splits bring few CUs (11 chunks, 2 units
-// 19.0 / 10.9, 128 22.4 / 18.8, 240 27.3 / 30.4; 19 chunks, 240 units 45.5 / 43.0).
+// 19.0 / 10.9, 128 22.4 / 18.8, 240 27.3 / 30.4; 19 chunks, 240 units 45.5 / 43.0;
+// d = 64, half the products, 11 chunks: 16 units 9.9 / 9.0, 60 11.8 / 13.0, 240
+// 12.9 / 16.2).
 struct TreeRoute {
     int shape, col_blocks, splits;
     size_t ws_bytes;
@@ -1016,7 +1018,7 @@ TreeRoute tree_route(long long units, long long cols, int d, int dtype, bool dra
     const int per = !wide ? 16 : cols <= 64 ? 64 : 128;
     const long long blocks = (cols + per - 1) / per, wgs = units * blocks;
     r.col_blocks = (int)blocks;
-    const int most = dtype == EVA_F32 ? (wgs > 128 ? 12 : 0) : wgs > 128 ? 20 : 12;
+    const int most = dtype == EVA_F32 ? (wgs > (d == 64 ? 32 : 128) ? 12 : 0) : wgs > 128 ? 20 : 12;
     if (!wide && wgs <= 256 && n_chunks > 4 && n_chunks <= most) r.shape = eva::kTreeNarrow12;
     r.splits = 1;
     if (r.shape != eva::kTreeNarrow12 && wgs < 256) {
