@@ -522,8 +522,8 @@ int eva_generate(const eva_rcache* cache, const void* q, const void* k, const vo
  *            tree's depths); NULL: 0 .. L - 1
  * Sums are fp32, each output is rounded once.  Outputs may not overlap x.
  * Errors: INVALID (sizes, null or misaligned pointers or rows, rot, eps not
- * finite or below 0), UNSUPPORTED (d, dtype, L above 2^30, B L or heads beyond
- * a grid).
+ * finite or below 0), UNSUPPORTED (d, dtype, B L above 2^26 - 64, more than 65535
+ * heads).
  */
 int eva_qk_norm_rope(const void* x, long long stride_b, long long stride_l, const void* q_weight, const void* k_weight,
                      const unsigned long long* turns, int rot, int interleaved, const int* start, const int* offsets,

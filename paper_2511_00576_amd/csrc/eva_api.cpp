@@ -821,6 +821,9 @@ int eva_generate(const eva_rcache* cache, const void* q, const void* k, const vo
 // ---------------------------------------------------------------------------
 
 // Checks what the forward and the backward share and lays down its parameters.
+// A wave a token: a launch takes fewer than 2^32 threads.
+static constexpr long long kMaxRopeTokens = (1 << 26) - 64;
+
 static int norm_rope_params(eva::NormRopeParams& p, const void* x, long long stride_b, long long stride_l,
                             const void* q_weight, const void* k_weight, const unsigned long long* turns, int rot,
                             int interleaved, const int* start, const int* offsets, float eps, int B, int H, int H_kv,
@@ -828,8 +831,7 @@ static int norm_rope_params(eva::NormRopeParams& p, const void* x, long long str
     if (B < 1 || H < 1 || H_kv < 1 || L < 1) return EVA_ERR_INVALID;
     const int st = supported(d, dtype);
     if (st != EVA_OK) return st;
-    if (L > kMaxLen || (long long)B * L > 0x7fffffffLL - 64 || (long long)H + 2LL * H_kv > 65535)
-        return EVA_ERR_UNSUPPORTED;
+    if ((long long)B * L > kMaxRopeTokens || (long long)H + 2LL * H_kv > 65535) return EVA_ERR_UNSUPPORTED;
     if (!x || !aligned16(x) || !aligned16(q_weight) || !aligned16(k_weight)) return EVA_ERR_INVALID;
     // every row starts on 16 bytes, and tokens do not overlap
     const long long per16 = dtype == EVA_BF16 ? 8 : 4;
@@ -876,7 +878,7 @@ int eva_qk_norm_rope(const void* x, long long stride_b, long long stride_l, cons
 }
 
 size_t eva_qk_norm_rope_backward_workspace_bytes(int B, int L, int d) {
-    if (B < 1 || L < 1 || d < 1 || (long long)B * L > 0x7fffffffLL - 64) return 0;
+    if (B < 1 || L < 1 || d < 1 || (long long)B * L > kMaxRopeTokens) return 0;
     return (size_t)eva::norm_rope_bwd_wgs(B * L) * 2 * d * sizeof(float);
 }
 
@@ -1037,7 +1039,7 @@ int tree_params(eva::TreeParams& p, TreeRoute& r, const eva::CacheView& v, int d
     const long long units = (long long)v.B * v.Hkv, cols = (long long)(v.H / v.Hkv) * T;
     if (cols > 0x7fffffffLL / 128) return EVA_ERR_UNSUPPORTED;
     r = tree_route(units, cols, d, dtype, drafted, n_chunks);
-    if ((units + 7) / 8 * 8 * r.col_blocks > 0x7fffffffLL || r.col_blocks > (1 << 27)) return EVA_ERR_UNSUPPORTED;
+    if ((units + 7) / 8 * 8 * r.col_blocks > 0xffffff) return EVA_ERR_UNSUPPORTED;  // 256 threads each, below 2^32
     p.c = v;
     p.n_tok = n_tok;
     p.active = active;

@@ -10,7 +10,9 @@
 //   dx = rstd (dn g - x^ mean(dn g x^))
 //
 // Both are bound by memory: every element is read once and written once (the
-// backward reads x and the gradients), about ten operations each.
+// backward reads x and the gradients), about ten operations each.  On MI355X,
+// bf16, H32/8 d128: 32768 tokens in 152 us, 5.3 TB/s; 16384 tokens forward and
+// backward 72 + 121 + 4.7 us, 5.1 TB/s (a copy of 1 GB runs at 5.1).
 //
 // A row is held by D / 16 lanes of 16 features, as two 8-feature chunks that
 // hold both members of the lane's eight pairs, so a turn stays in the lane;

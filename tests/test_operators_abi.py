@@ -47,7 +47,7 @@ def rope_backward(lib, **kw):
     (dict(turns=ctypes.c_void_p(0x10004)), INVALID), (dict(inter=2), INVALID),
     (dict(eps=-1e-6), INVALID), (dict(eps=float("nan")), INVALID), (dict(eps=float("inf")), INVALID),
     (dict(d=96), UNSUPPORTED), (dict(dtype=2), UNSUPPORTED), (dict(L=2 ** 30 + 1), UNSUPPORTED),
-    (dict(B=4, L=2 ** 30), UNSUPPORTED), (dict(H=65000, H_kv=300), UNSUPPORTED),
+    (dict(B=4, L=2 ** 30), UNSUPPORTED), (dict(B=1, L=2 ** 26 - 63), UNSUPPORTED), (dict(H=65000, H_kv=300), UNSUPPORTED),
 ])
 def test_norm_rope_rejects(lib, call, kw, code):
     assert call(lib, **kw) == code
