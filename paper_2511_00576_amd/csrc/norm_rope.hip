@@ -14,8 +14,8 @@
 // bf16, H32/8 d128: 32768 tokens in 152 us, 5.3 TB/s; 16384 tokens forward and
 // backward 72 + 121 + 4.7 us, 5.1 TB/s (a copy of 1 GB runs at 5.1).
 //
-// A row is held by D / 16 lanes of 16 features, as two 8-feature chunks that
-// hold both members of the lane's eight pairs, so a turn stays in the lane;
+// A row is held by D / 16 lanes of 16 features, in pieces of 16 bytes that hold
+// both members of the lane's eight pairs, so a turn stays in the lane;
 // a wave works on 1024 / D rows of one token at a time and computes the
 // token's angles once for all its heads.  Where the queries' heads would leave
 // half of the lanes idle or more, a wave holds several tokens.  Angles are whole numbers: p times
@@ -30,31 +30,15 @@ namespace {
 
 constexpr int kNormRopeWaves = 4;
 
-__device__ __forceinline__ void load8(const bf16* p, float out[8]) {
-    const u32x4 w = *reinterpret_cast<const u32x4*>(p);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        out[2 * i] = bf16_lo(w[i]);
-        out[2 * i + 1] = bf16_hi(w[i]);
-    }
-}
-__device__ __forceinline__ void load8(const float* p, float out[8]) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const floatx4 w = *reinterpret_cast<const floatx4*>(p + 4 * h);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) out[4 * h + i] = w[i];
-    }
-}
-// A lane's 16 features of a row as they lie in memory.
+// A lane's 16 features of a row as they lie in memory, in 16-byte pieces.
 template <typename T>
 struct RawRow {
-    static constexpr int N = (int)sizeof(T);  // 16-byte pieces
+    static constexpr int N = (int)sizeof(T);
     u32x4 w[N];
-    __device__ __forceinline__ void load(const T* row, int f0, int f1) {
+    template <typename Row>
+    __device__ __forceinline__ void load(const T* row, const Row& r) {
 #pragma unroll
-        for (int i = 0; i < N; ++i)
-            w[i] = *reinterpret_cast<const u32x4*>(row + (i < N / 2 ? f0 : f1) + i % (N / 2) * (16 / sizeof(T)));
+        for (int i = 0; i < N; ++i) w[i] = *reinterpret_cast<const u32x4*>(row + r.piece(i));
     }
     __device__ __forceinline__ void values(float (&x)[16]) const {
 #pragma unroll
@@ -66,25 +50,29 @@ struct RawRow {
         }
     }
 };
-__device__ __forceinline__ void store8(bf16* p, const float x[8]) {
+__device__ __forceinline__ void store_piece(bf16* p, const float* x) {
     *reinterpret_cast<u32x4*>(p) = u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
                                          pack_bf16x2(x[6], x[7])};
 }
-__device__ __forceinline__ void store8(float* p, const float x[8]) {
+__device__ __forceinline__ void store_piece(float* p, const float* x) {
     *reinterpret_cast<floatx4*>(p) = floatx4{x[0], x[1], x[2], x[3]};
-    *reinterpret_cast<floatx4*>(p + 4) = floatx4{x[4], x[5], x[6], x[7]};
 }
 
-// Where a lane's two chunks lie and how its pairs are formed.
+// Where a lane's pieces lie and how its pairs are formed.  fp32 pieces lie side by
+// side across the lanes that are turned, and across the others, so that an
+// instruction reads whole lines: 8192 tokens of H32/8 d128 90 us, with a lane's 16
+// features side by side 117 (forward and backward 215 / 252; H16/2 d64 191 / 187).
+// (bf16 with adjacent pairs, and what is not turned, two pieces side by side in a
+// lane: half of a line each.)
 // ADJ: pairs are adjacent features.  PACK: a wave holds 1 << a.pack tokens, each
 // with all its heads of a kind in one sweep; else one token.
-template <int D, bool ADJ, bool PACK>
+template <int D, typename T, bool ADJ, bool PACK>
 struct LaneRow {
     static constexpr int kLanes = D / 16;           // lanes per row
     static constexpr int kRows = 64 / kLanes;       // rows per wave
     int c, sub;                                     // place in the row, row in the wave
     int h, t;                                       // its head in a sweep, its token in the wave
-    int f0, f1;                                     // first feature of the chunks
+    int f0, f1;                                     // bf16: first feature of the pieces; fp32: and their distance
     bool turned;                                    // its pairs are turned
     __device__ LaneRow(const NormRopeParams& a) {
         const int lane = threadIdx.x & 63;
@@ -97,26 +85,41 @@ struct LaneRow {
             t = sub / (kRows >> a.pack);
         }
         turned = 16 * c < a.rot;
-        // halves: pair i is (i, i + rot / 2), so chunk c goes with chunk c + rot / 16;
-        // the features that are not turned, and adjacent pairs, lie side by side
-        const bool halves = turned && !ADJ;
-        f0 = 8 * (halves ? c : 2 * c);
-        f1 = 8 * (halves ? c + a.rot / 16 : 2 * c + 1);
+        // halves: pair i is (i, i + rot / 2), whose members lie in pieces half of the
+        // lane's pieces apart
+        if constexpr (sizeof(T) == 2) {
+            const bool halves = turned && !ADJ;
+            f0 = 8 * (halves ? c : 2 * c);
+            f1 = 8 * (halves ? c + a.rot / 16 : 2 * c + 1);
+        } else {
+            f0 = turned ? 4 * c : a.rot + 4 * (c - a.rot / 16);
+            f1 = 4 * (turned ? a.rot / 16 : kLanes - a.rot / 16);
+        }
+    }
+    // First feature of piece i.
+    __device__ __forceinline__ int piece(int i) const {
+        if constexpr (sizeof(T) == 2) return i ? f1 : f0;
+        return f0 + i * f1;
+    }
+    // The lane's element i is this feature; its pair j has this frequency.
+    __device__ __forceinline__ int feature(int i) const { return piece(i / (16 / (int)sizeof(T))) + i % (16 / (int)sizeof(T)); }
+    __device__ __forceinline__ int frequency(int j) const {
+        if constexpr (sizeof(T) == 2) return 8 * c + j;
+        return ADJ ? (f0 + (j >> 1) * f1) / 2 + (j & 1) : f0 + (j >> 2) * f1 + (j & 3);
     }
     __device__ float sum(float x) const {
 #pragma unroll
         for (int off = 1; off < kLanes; off <<= 1) x += __shfl_xor(x, off, 64);
         return x;
     }
-    template <typename T>
     __device__ void load(const T* row, float (&x)[16]) const {
-        load8(row + f0, x);
-        load8(row + f1, x + 8);
+        RawRow<T> w;
+        w.load(row, *this);
+        w.values(x);
     }
-    template <typename T>
     __device__ void store(T* row, const float (&x)[16]) const {
-        store8(row + f0, x);
-        store8(row + f1, x + 8);
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T); ++i) store_piece(row + piece(i), x + i * (16 / (int)sizeof(T)));
     }
     // SIGN 1: by the angles, -1: back
     template <int SIGN>
@@ -154,7 +157,7 @@ __device__ __forceinline__ void angles(const NormRopeParams& a, const Row& r, in
     const int b = tok / a.fL, l = tok - b * a.fL.d;
     const long long pos = (long long)(a.start ? a.start[b] : 0) + (a.offsets ? a.offsets[tok] : l);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) cos_sin((unsigned long long)pos * a.turns[8 * r.c + j], cs[j], sn[j]);
+    for (int j = 0; j < 8; ++j) cos_sin((unsigned long long)pos * a.turns[r.frequency(j)], cs[j], sn[j]);
 }
 
 // Sweeps of a token: kRows heads each, queries first, then keys, then values.
@@ -172,7 +175,7 @@ struct Sweeps {
 // 1 << a.pack tokens.
 template <int D, typename T, bool ADJ, bool PACK>
 __global__ __launch_bounds__(kNormRopeWaves * 64) void norm_rope_kernel(NormRopeParams a) {
-    const LaneRow<D, ADJ, PACK> r(a);
+    const LaneRow<D, T, ADJ, PACK> r(a);
     int tok = blockIdx.x * kNormRopeWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if constexpr (PACK) tok = (tok << a.pack) + r.t;
     if (tok >= a.tokens) return;  // (all lanes of a row together)
@@ -189,7 +192,7 @@ __global__ __launch_bounds__(kNormRopeWaves * 64) void norm_rope_kernel(NormRope
                      (s - (kind == 0 ? 0 : kind == 1 ? sw.q : sw.k)) * r.kRows + r.h};
     };
     RawRow<T> raw;
-    auto request = [&](const Sweep& w) { raw.load(xt + (size_t)(w.first + min(w.h, w.heads - 1)) * D, r.f0, r.f1); };
+    auto request = [&](const Sweep& w) { raw.load(xt + (size_t)(w.first + min(w.h, w.heads - 1)) * D, r); };
     // rows are requested a sweep ahead, the first before the angles
     Sweep w = sweep(blockIdx.y);
     request(w);
@@ -227,7 +230,7 @@ __global__ __launch_bounds__(kNormRopeWaves * 64) void norm_rope_kernel(NormRope
 // bits every time.
 template <int D, typename T, bool ADJ, bool PACK>
 __global__ __launch_bounds__(kNormRopeWaves * 64, 3) void norm_rope_bwd_kernel(NormRopeParams a) {
-    const LaneRow<D, ADJ, PACK> r(a);
+    const LaneRow<D, T, ADJ, PACK> r(a);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Sweeps sw(a, r.kRows);
     float dg[2][16] = {};
@@ -285,7 +288,7 @@ __global__ __launch_bounds__(kNormRopeWaves * 64, 3) void norm_rope_bwd_kernel(N
             float x = dg[n][i];
 #pragma unroll
             for (int off = r.kLanes; off < 64; off <<= 1) x += __shfl_xor(x, off, 64);
-            if (r.sub == 0) part[wave][n][(i < 8 ? r.f0 : r.f1 - 8) + i] = x;
+            if (r.sub == 0) part[wave][n][r.feature(i)] = x;
         }
     __syncthreads();
     for (int e = threadIdx.x; e < 2 * D; e += blockDim.x) {

@@ -523,7 +523,8 @@ def qk_norm_rope(x, H: int, Hkv: int, turns=None, q_weight=None, k_weight=None, 
     args, dev, B, L, d = _norm_rope_args(x, H, Hkv, turns, q_weight, k_weight, eps, start, offsets, interleaved)
     code = _dtype_code(x)
     if out is None:
-        Q, K, V = x.new_empty((B, H, L, d)), x.new_empty((B, Hkv, L, d)), x.new_empty((B, Hkv, L, d))
+        Q, K = x.new_empty((B, H, L, d)), x.new_empty((B, Hkv, L, d))
+        V = torch.empty_like(K)
         q, k, v = Q.data_ptr(), K.data_ptr(), V.data_ptr()
     else:
         Q, K, V = out
