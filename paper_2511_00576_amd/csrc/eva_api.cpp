@@ -1005,10 +1005,11 @@ int row_chunks(int window, int max_tok, int W, int C, int S_max, int keys) {
 // with the join, 128 9.7 / 12.6, 256 11.1 / 12.8; trees of 20 chunks, 2 units 14.2 /
 // 11.2, 128 17.6 / 17.3, 240 18.8 / 22.8, bf16 11.3 / 9.2, 16.9 / 16.0, 17.9 / 22.0;
 // 35 chunks, 136 units 27.3 / 25.1).  fp32 products are slow enough to bound a CU of
-// 12 waves: only for one round and where splits bring few CUs (11 chunks, 2 units
-// 19.0 / 10.9, 128 22.4 / 18.8, 240 27.3 / 30.4; 19 chunks, 240 units 45.5 / 43.0;
-// d = 64, half the products, 11 chunks: 16 units 9.9 / 9.0, 60 11.8 / 13.0, 240
-// 12.9 / 16.2).
+// 12 waves: of 128 features only for one round and where splits bring few CUs (11
+// chunks, 2 units 19.0 / 10.9, 128 22.4 / 18.8, 240 27.3 / 30.4; 19 chunks, 240 units
+// 45.5 / 43.0), of 64, half the products, sooner (5 chunks, 40 units 8.2 / 9.1; 11,
+// 40 10.2 / 9.1 and 128 11.8 / 12.7; 19, 80 15.2 / 13.0 and 128 15.3 / 16.5; 13, 60
+// 11.2 / 10.4, but 11.8 / 13.0 where the host launches each call).
 struct TreeRoute {
     int shape, col_blocks, splits;
     size_t ws_bytes;
@@ -1020,7 +1021,8 @@ TreeRoute tree_route(long long units, long long cols, int d, int dtype, bool dra
     const int per = !wide ? 16 : cols <= 64 ? 64 : 128;
     const long long blocks = (cols + per - 1) / per, wgs = units * blocks;
     r.col_blocks = (int)blocks;
-    const int most = dtype == EVA_F32 ? (wgs > (d == 64 ? 32 : 128) ? 12 : 0) : wgs > 128 ? 20 : 12;
+    int most = wgs > 128 ? 20 : 12;  // chunks
+    if (dtype == EVA_F32) most = d == 64 ? (wgs > 96 ? 20 : wgs > 32 ? 16 : 0) : wgs > 128 ? 12 : 0;
     if (!wide && wgs <= 256 && n_chunks > 4 && n_chunks <= most) r.shape = eva::kTreeNarrow12;
     r.splits = 1;
     if (r.shape != eva::kTreeNarrow12 && wgs < 256) {
