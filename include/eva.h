@@ -515,6 +515,7 @@ int eva_generate(const eva_rcache* cache, const void* q, const void* k, const vo
  *   turns    device [rot / 2]: the frequencies in 2^-64 turns per position
  *            (2^64 theta_i / 2 pi, wrapping), so the angle of any position is
  *            exact: a whole product modulo 2^64
+ *   H, H_kv  any numbers of heads (H need not be a multiple of H_kv here)
  *   rot      0 .. d, a multiple of 16 (0: no rotation, turns may be NULL)
  *   start    device int32 [B], the position of each sequence's first token
  *            (a ragged cache's n_tok, say); NULL: 0

@@ -17,7 +17,7 @@
 // A row is held by D / 16 lanes of 16 features, in pieces of 16 bytes that hold
 // both members of the lane's eight pairs, so a turn stays in the lane;
 // a wave works on 1024 / D rows of one token at a time and computes the
-// token's angles once for all its heads.  Where the queries' heads would leave
+// token's angles once for all its heads.  Where the heads of every kind would leave
 // half of the lanes idle or more, a wave holds several tokens.  Angles are whole numbers: p times
 // the frequency in 2^-64 turns, modulo 2^64, is exact to 2^-64 p turns at any
 // position, where a product in fp32 is off by radians from 2^24 on.
@@ -330,21 +330,23 @@ __global__ __launch_bounds__(1024) void norm_rope_sum_kernel(const float* __rest
 
 }  // namespace
 
-// log2 of the tokens a wave holds: as many as fit with all their query heads.
+// log2 of the tokens a wave holds: as many as fit with all their heads of the kind
+// that has more (a sweep of a packed wave holds all of a kind).
 // (us a launch on MI355X, several tokens a wave / one: bf16 d64 H1 B28 L1300 8.6 /
 // 36.5 and backward 14.7 / 44.8, d128 H4/1 B16 L1300 17.1 / 23.8 and 28 / 44, fp32
 // d64 H8/2 B16 L1300 32.0 / 36.5 and 42.7 / 67.)
 template <int D>
-int tokens_log2(int H) {
+int tokens_log2(int H, int Hkv) {
+    const int heads = H > Hkv ? H : Hkv;
     int n = 0;
-    while (H << (n + 1) <= 1024 / D) ++n;
+    while (heads << (n + 1) <= 1024 / D) ++n;
     return n;
 }
 
 template <int D, typename T>
 hipError_t launch_norm_rope(NormRopeParams p, hipStream_t stream) {
     constexpr int rows = 1024 / D;
-    p.pack = tokens_log2<D>(p.H);
+    p.pack = tokens_log2<D>(p.H, p.Hkv);
     const int sweeps = (p.H + rows - 1) / rows + 2 * ((p.Hkv + rows - 1) / rows);
     const int per = kNormRopeWaves << p.pack, wgs = (p.tokens + per - 1) / per;
     // few tokens: their heads over workgroups, until there are four waves a CU
@@ -360,7 +362,7 @@ hipError_t launch_norm_rope(NormRopeParams p, hipStream_t stream) {
 
 template <int D, typename T>
 hipError_t launch_norm_rope_backward(NormRopeParams p, hipStream_t stream) {
-    p.pack = tokens_log2<D>(p.H);
+    p.pack = tokens_log2<D>(p.H, p.Hkv);
     const int wgs = norm_rope_bwd_wgs((p.tokens + (1 << p.pack) - 1) >> p.pack);
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(wgs), dim3(kNormRopeWaves * 64), 0, stream, p); };
     if (p.interleaved)
