@@ -671,7 +671,7 @@ __global__ __launch_bounds__(256) void decode_combine_kernel(DecodeParams a) {
                 }
                 mx = fmaxf(mx, m[i]);
             }
-            if (mx == -INFINITY) continue;
+            // no maximum yet: no weight either, but a sum of NaN (all its keys were) stays one
             const float keep = M == -INFINITY ? 0.f : fast_exp2(M - mx);
             num *= keep;
             den *= keep;

@@ -57,3 +57,15 @@ def test_trees(kind):
     if kind == "e4m3":
         q = q[:, :, 0].contiguous()
         check(eva.qdecode_step(cache, q), eva.qdecode_step(cache, q, use_workspace=False), "decode")
+
+
+def test_ragged_and_uniform_decode():
+    rows = prompt(torch.bfloat16)
+    q = inputs.normal((B, H, D), 9, torch.bfloat16).cuda()
+    cache = eva.RaggedCache(B, H, HKV, D, W, C, max_tokens=N + 8, fill=0.0)
+    eva.rcache_fill(cache, *rows, torch.tensor([N], dtype=torch.int32, device="cuda"))
+    assert cache.ws.numel() // (B * HKV * 16 * (D + 2)) > 8, "the shape must split its rows more than eight times"
+    check(eva.rdecode_step(cache, q), eva.rdecode_step(cache, q, use_workspace=False), "ragged")
+    cache = eva.Cache(B, H, HKV, D, W, C, max_tokens=N + 8, fill=0.0)
+    eva.cache_fill(cache, *rows)
+    check(eva.decode_step(cache, q), eva.decode_step(cache, q, use_workspace=False), "uniform")
