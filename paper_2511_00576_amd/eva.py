@@ -452,6 +452,8 @@ _functions = {}
 def _call(dev, name, *args):
     """Call lib.<name>(*args, stream) on the current stream of device `dev` (its
     index), with that device current."""
+    if dev < 0:  # (operands on the device of a cache in host memory)
+        raise RuntimeError("EVA kernels run on the GPU only: tensors must be on a ROCm device")
     fn = _functions.get(name)
     if fn is None:
         fn = _functions[name] = getattr(_lib.load(), name)
