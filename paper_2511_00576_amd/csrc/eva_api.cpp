@@ -1186,25 +1186,33 @@ size_t eva_qdecode_workspace_bytes(const eva_qcache* cache) {
     return tree_route((long long)cache->B * cache->H_kv, cache->H / cache->H_kv, cache->d, EVA_BF16, false, q_chunks(cache)).ws_bytes;
 }
 
-int eva_qdecode_step(const eva_qcache* cache, const void* q, void* o, const int* active, void* ws, size_t ws_bytes,
-                     void* stream) {
-    int st = check_qcache(cache);
+static int qdecode_params(eva::TreeParams& p, const eva_qcache* cache, const void* q, void* o, const int* active, void* ws,
+                          size_t ws_bytes) {
+    const int st = check_qcache(cache);
     if (st != EVA_OK) return st;
-    eva::TreeParams p{};
     p.qc = qview_of(cache);
     TreeRoute r;
-    st = tree_params(p, r, qgeometry_of(cache), cache->d, EVA_BF16, cache->n_tok, cache->max_tok, active, q, o, 1, false,
-                     q_chunks(cache), ws, ws_bytes);
+    return tree_params(p, r, qgeometry_of(cache), cache->d, EVA_BF16, cache->n_tok, cache->max_tok, active, q, o, 1, false,
+                       q_chunks(cache), ws, ws_bytes);
+}
+
+int eva_qdecode_step(const eva_qcache* cache, const void* q, void* o, const int* active, void* ws, size_t ws_bytes,
+                     void* stream) {
+    eva::TreeParams p{};
+    const int st = qdecode_params(p, cache, q, o, active, ws, ws_bytes);
     if (st != EVA_OK) return st;
     return launch_q(p, cache->d, stream);
 }
 
 int eva_qappend_decode(const eva_qcache* cache, const void* q, const void* k_new, const void* v_new, void* o,
                        const int* active, void* ws, size_t ws_bytes, void* stream) {
-    if (!q || !o || !aligned16(q) || !aligned16(o)) return EVA_ERR_INVALID;
-    const int st = eva_qcache_append(cache, k_new, v_new, active, stream);
+    // what the decode refuses is refused before the append
+    eva::TreeParams p{};
+    int st = qdecode_params(p, cache, q, o, active, ws, ws_bytes);
     if (st != EVA_OK) return st;
-    return eva_qdecode_step(cache, q, o, active, ws, ws_bytes, stream);
+    st = eva_qcache_append(cache, k_new, v_new, active, stream);
+    if (st != EVA_OK) return st;
+    return launch_q(p, cache->d, stream);
 }
 
 size_t eva_qtree_workspace_bytes(const eva_qcache* cache, int T) {

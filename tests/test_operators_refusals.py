@@ -36,3 +36,27 @@ def test_caches_in_host_memory_are_refused(name):
     for cache in (quant, ragged) if name in ("tree", "path") else (quant,):
         with pytest.raises(RuntimeError, match="ROCm device"):
             calls[name](cache)
+
+
+# ---- the C entries: addresses that are never dereferenced -------------------------
+FAKE = ctypes.c_void_p(0x10000)
+INVALID, UNSUPPORTED = _lib.EVA_ERR_INVALID, _lib.EVA_ERR_UNSUPPORTED
+
+
+def quant_struct(**kw):
+    a = dict(B=2, H=4, H_kv=2, d=64, W=8, C=4, window=0, R=64, S_max=64, max_tok=100, n_tok=0x50000, arrive=0x60000,
+             k_ring=0x10000, vt_ring=0x20000, k_sum=0x30000, vt_sum=0x40000, k_ring_exp=0x70000, v_ring_exp=0x80000,
+             k_sum_exp=0x90000, v_sum_exp=0xa0000)
+    a.update(kw)
+    return _lib.EvaQCacheStruct(**a)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(H=2 ** 30, H_kv=2),             # more columns than a launch has
+    dict(B=30000, H=2 ** 17, H_kv=2),    # more workgroups
+])
+def test_append_and_decode_is_refused_before_the_append(kw):
+    # (an append that is enqueued answers EVA_ERR_HIP where there is no GPU)
+    lib, c = _lib.load(), ctypes.byref(quant_struct(**kw))
+    assert lib.eva_qdecode_step(c, FAKE, FAKE, None, None, 0, None) == UNSUPPORTED
+    assert lib.eva_qappend_decode(c, FAKE, FAKE, FAKE, FAKE, None, None, 0, None) == UNSUPPORTED
