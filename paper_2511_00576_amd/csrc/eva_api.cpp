@@ -16,6 +16,7 @@ using eva::bf16;
 namespace {
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
 int supported(int d, int dtype) {
     if (dtype != EVA_BF16 && dtype != EVA_F32) return EVA_ERR_UNSUPPORTED;
@@ -839,7 +840,7 @@ static int norm_rope_params(eva::NormRopeParams& p, const void* x, long long str
     if (stride_b < 0 || stride_l < 0) return EVA_ERR_INVALID;
     if (rot < 0 || rot > d || rot % 16 != 0 || (rot > 0 && !turns) || (interleaved != 0 && interleaved != 1))
         return EVA_ERR_INVALID;
-    if ((reinterpret_cast<uintptr_t>(turns) & 7u) != 0) return EVA_ERR_INVALID;
+    if ((reinterpret_cast<uintptr_t>(turns) & 7u) != 0 || !aligned4(start) || !aligned4(offsets)) return EVA_ERR_INVALID;
     if (!(eps >= 0.f) || eps > 1e30f) return EVA_ERR_INVALID;
     p.x = x;
     p.stride_b = stride_b;
@@ -894,7 +895,8 @@ int eva_qk_norm_rope_backward(const void* x, long long stride_b, long long strid
     const void* must[] = {dQ, dK, dV, dx};
     for (const void* ptr : must)
         if (!ptr || !aligned16(ptr)) return EVA_ERR_INVALID;
-    if ((q_weight && !dq_weight) || (k_weight && !dk_weight)) return EVA_ERR_INVALID;
+    if ((q_weight && (!dq_weight || !aligned4(dq_weight))) || (k_weight && (!dk_weight || !aligned4(dk_weight))))
+        return EVA_ERR_INVALID;
     if (q_weight || k_weight) {
         if (!ws || !aligned16(ws)) return EVA_ERR_INVALID;
         if (ws_bytes < eva_qk_norm_rope_backward_workspace_bytes(B, L, d)) return EVA_ERR_CAPACITY;
@@ -1068,7 +1070,7 @@ int tree_params(eva::TreeParams& p, TreeRoute& r, const eva::CacheView& v, int d
 int tree_nodes(eva::TreeParams& p, const void* k, const void* v, const int* parents, const int* n_nodes, int T, int W, int window) {
     const int st = check_nodes(T, W);
     if (st != EVA_OK) return st;
-    if (!k || !v || !parents || !aligned16(k) || !aligned16(v)) return EVA_ERR_INVALID;
+    if (!k || !v || !parents || !aligned16(k) || !aligned16(v) || !aligned4(parents)) return EVA_ERR_INVALID;
     // a blocked window's next block would need summaries of drafted tokens
     if (window == EVA_WINDOW_BLOCKED && T > 1) return EVA_ERR_UNSUPPORTED;
     p.k = k;

@@ -60,3 +60,29 @@ def test_append_and_decode_is_refused_before_the_append(kw):
     lib, c = _lib.load(), ctypes.byref(quant_struct(**kw))
     assert lib.eva_qdecode_step(c, FAKE, FAKE, None, None, 0, None) == UNSUPPORTED
     assert lib.eva_qappend_decode(c, FAKE, FAKE, FAKE, FAKE, None, None, 0, None) == UNSUPPORTED
+
+
+OFF4 = ctypes.c_void_p(0x10002)  # not on four bytes
+
+
+@pytest.mark.parametrize("kind", ["r", "q"])
+def test_misaligned_parents_are_refused(kind):
+    lib = _lib.load()
+    if kind == "q":
+        c = quant_struct()
+    else:
+        c = _lib.EvaRCacheStruct(B=2, H=4, H_kv=2, d=64, W=8, C=4, dtype=_lib.EVA_BF16, window=0, R=32, S_max=32, max_tok=100,
+                                 n_tok=0x50000, arrive=0x60000, k_ring=0x10000, vt_ring=0x20000, k_sum=0x30000, vt_sum=0x40000)
+    tree = getattr(lib, f"eva_{kind}tree_attention")
+    assert tree(ctypes.byref(c), FAKE, FAKE, FAKE, OFF4, None, FAKE, 4, None, None, 0, None) == INVALID
+
+
+@pytest.mark.parametrize("start,offsets,dgq,dgk", [(OFF4, None, FAKE, FAKE), (None, OFF4, FAKE, FAKE), (None, None, OFF4, FAKE),
+                                                   (None, None, FAKE, OFF4)])
+def test_misaligned_operands_of_head_norms_are_refused(start, offsets, dgq, dgk):
+    lib = _lib.load()
+    head = (FAKE, 0, 512, FAKE, FAKE, FAKE, 64, 0, start, offsets, 1e-6)
+    size = (1, 4, 2, 64, 64, _lib.EVA_BF16)
+    if start or offsets:
+        assert lib.eva_qk_norm_rope(*head, FAKE, FAKE, FAKE, *size, None) == INVALID
+    assert lib.eva_qk_norm_rope_backward(*head, FAKE, FAKE, FAKE, FAKE, dgq, dgk, FAKE, 1 << 30, *size, None) == INVALID
