@@ -1009,9 +1009,21 @@ int row_chunks(int window, int max_tok, int W, int C, int S_max, int keys) {
 // 35 chunks, 136 units 27.3 / 25.1).  fp32 products are slow enough to bound a CU of
 // 12 waves: of 128 features only for one round and where splits bring few CUs (11
 // chunks, 2 units 19.0 / 10.9, 128 22.4 / 18.8, 240 27.3 / 30.4; 19 chunks, 240 units
-// 45.5 / 43.0), of 64, half the products, sooner (5 chunks, 40 units 8.2 / 9.1; 11,
-// 40 10.2 / 9.1 and 128 11.8 / 12.7; 19, 80 15.2 / 13.0 and 128 15.3 / 16.5; 13, 60
-// 11.2 / 10.4, but 11.8 / 13.0 where the host launches each call).
+// 45.5 / 43.0).  Of 64 features, half the products, by what the splits would bring:
+// two a row (up to 8 chunks) never pay for their join; three do while all their
+// workgroups have a CU; past 128 workgroups no split brings enough (12 waves / 4
+// split, columns: units of 16 columns, W = 32 (chunks - 3)):
+//   units      8           40          72          96          128         160
+//   5   8.8 /  9.4  8.9 /  9.6  8.9 /  9.7  9.0 / 10.0  9.8 / 11.7 10.1 / 13.4
+//   8   9.2 /  9.3  9.4 /  9.5 10.1 / 11.0 10.6 / 11.8 10.6 / 12.3 10.7 / 13.8
+//   10 10.6 /  9.4 11.5 / 11.2 11.7 / 11.4 11.8 / 13.3 12.0 / 13.4 12.0 / 13.9
+//   12 11.1 /  9.4 11.4 / 10.3 12.5 / 12.0 12.6 / 13.6 12.7 / 13.7 12.8 / 14.2
+//   13 12.3 /  9.6 13.2 / 10.9 13.9 / 13.1 14.0 / 13.5 14.1 / 13.9 14.3 / 15.7
+//   16 12.3 /  9.4 13.5 / 11.2 14.2 / 13.4 14.3 / 13.6 14.4 / 14.2 14.6 / 16.7
+//   20 14.4 /  9.4 15.9 / 11.8 16.0 / 13.6 16.1 / 14.1 16.3 / 16.4 16.5 / 18.2
+// Over 25 numbers of units from 1 to 240 and 5 to 20 chunks the rule's side is at most
+// 3.5% behind the other, but for 128 x 18, 7%.  (Captured, as all times here; a call
+// that is not pays about 1 us of host time for the join's launch.)
 struct TreeRoute {
     int shape, col_blocks, splits;
     size_t ws_bytes;
@@ -1024,7 +1036,7 @@ TreeRoute tree_route(long long units, long long cols, int d, int dtype, bool dra
     const long long blocks = (cols + per - 1) / per, wgs = units * blocks;
     r.col_blocks = (int)blocks;
     int most = wgs > 128 ? 20 : 12;  // chunks
-    if (dtype == EVA_F32) most = d == 64 ? (wgs > 96 ? 20 : wgs > 32 ? 16 : 0) : wgs > 128 ? 12 : 0;
+    if (dtype == EVA_F32) most = d == 64 ? (wgs > 128 ? 20 : wgs > 80 ? 12 : 8) : wgs > 128 ? 12 : 0;
     if (!wide && wgs <= 256 && n_chunks > 4 && n_chunks <= most) r.shape = eva::kTreeNarrow12;
     r.splits = 1;
     if (r.shape != eva::kTreeNarrow12 && wgs < 256) {
