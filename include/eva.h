@@ -521,7 +521,9 @@ int eva_generate(const eva_rcache* cache, const void* q, const void* k, const vo
  *            (a ragged cache's n_tok, say); NULL: 0
  *   offsets  device int32 [B][L], each token's distance from it (a drafted
  *            tree's depths); NULL: 0 .. L - 1
- * Sums are fp32, each output is rounded once.  Outputs may not overlap x.
+ * Sums are fp32, each output is rounded once (of a row whose squares' sum passes
+ * fp32's range, entries of some 1e18 and more, the norm makes zeros).  Outputs may not
+ * overlap x.
  * Errors: INVALID (sizes, null or misaligned pointers or rows, rot, eps not
  * finite or below 0), UNSUPPORTED (d, dtype, B L above 2^26 - 64, more than 65535
  * heads).
@@ -599,10 +601,17 @@ int eva_rappend_path(const eva_rcache* cache, const void* k, const void* v, cons
  * power of two for each row, half the bytes of a bf16 one.  A row x is held as
  * d codes and one byte e:
  *     x_i ~ code_i 2^(e - 127),  code_i = e4m3(x_i 2^(127 - e)) (ties to even),
- * e the smallest that brings the row's largest finite magnitude to 448 or
- * below (127 for a row of zeros; 1 .. 246).  So every entry above 2^-15 of the
- * row's largest is off by 2^-4 of itself at most.  Entries that are not finite
- * are held as NaN.  q, k, v, o are bf16.
+ * e the smallest, of 1 .. 246, that brings the row's largest finite magnitude to
+ * 448 or below (127 for a row of zeros).  An entry is off by 2^-4 of itself at
+ * most, or by 2^-10 2^(e - 127), half of the smallest code: the former for every
+ * entry from 2^-13 of the row's largest on, the latter below 2^-17 of it (rows
+ * whose largest is below 2^-118, where e has no smaller value, apart).
+ * Entries that are not finite are held as NaN, and so are finite ones above
+ * 464 2^119 = 3.08e38, next to the type's largest (3.39e38), which no code reaches
+ * at e = 246 (above 448 2^119 they are held as that): a greater e would let the
+ * softmax's unscaled weights, up to 2^8, overflow with the scale.
+ * q, k, v, o are bf16; as with EVA_BF16 caches the softmax weights are rounded to
+ * bf16 before the weighted sum of values, all sums are fp32.
  *   k_ring  [B][H_kv][R][d]            codes, row per slot
  *   vt_ring [B][H_kv][R/16][d][16]     codes: slot s, feature f at [s/16][f][s%16]
  *   k_sum   [B][H_kv][S_max][d]

@@ -834,7 +834,7 @@ static int norm_rope_params(eva::NormRopeParams& p, const void* x, long long str
     if (st != EVA_OK) return st;
     if ((long long)B * L > kMaxRopeTokens || (long long)H + 2LL * H_kv > 65535) return EVA_ERR_UNSUPPORTED;
     if (!x || !aligned16(x) || !aligned16(q_weight) || !aligned16(k_weight)) return EVA_ERR_INVALID;
-    // every row starts on 16 bytes, and tokens do not overlap
+    // every row starts on 16 bytes (a stride of 0 repeats a row)
     const long long per16 = dtype == EVA_BF16 ? 8 : 4;
     if (stride_b % per16 != 0 || stride_l % per16 != 0) return EVA_ERR_INVALID;
     if (stride_b < 0 || stride_l < 0) return EVA_ERR_INVALID;

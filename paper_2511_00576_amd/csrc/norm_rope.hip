@@ -137,7 +137,10 @@ struct LaneRow {
 
 // cos and sin of t 2^-64 turns.  The nearest quarter turn is taken off the whole
 // number, exactly; what is left, at most pi / 4, goes into the Taylor series to
-// x^9 and x^10, whose next terms are below 2^-29 and 2^-35.
+// x^9 and x^10, whose next terms are below 2^-29 and 2^-33.  Beside the series'
+// own roundings x is off by the turns below 2^-32 (2 pi 2^-32 = 0.03 of 2^-24), the
+// rounding of a whole number of 30 bits and that of the product, 2^-24 of pi / 4 each: sine
+// and cosine within 4 x 2^-24.
 __device__ __forceinline__ void cos_sin(unsigned long long t, float& c, float& s) {
     const uint32_t hi = (uint32_t)(t >> 32);
     const uint32_t quarter = (hi + 0x20000000u) >> 30;

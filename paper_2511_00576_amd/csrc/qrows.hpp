@@ -2,9 +2,12 @@
 // value = code 2^(byte - 127).  The exponent is the smallest whose power of
 // two brings the row's largest finite magnitude to 448, e4m3's largest value,
 // or below.  A power of two scales exactly both ways, so a code differs from
-// the row's value by its one rounding, and rows of the same values have the same codes wherever
-// they are quantised; a row's small entries lose nothing either, since the
-// codes have exponents of their own (2^-6 and less of 448 becomes subnormal).
+// the row's value by its one rounding, half a step (2^-4 of an entry: 3 mantissa
+// bits), and rows of the same values have the same codes wherever they are
+// quantised; a row's small entries lose nothing more, since the codes have
+// exponents of their own, until they are subnormal, below 2^-6 of the row's power
+// of two, where half a step is 2^-10 of that (so from 2^-13 of the row's largest, which
+// lies in (224, 448], every code is a normal one).
 #pragma once
 
 #include "eva_device.hpp"
@@ -22,7 +25,10 @@ __host__ __device__ __forceinline__ size_t qt_index(int f, int r) {
 
 __device__ __forceinline__ bool is_finite(float x) { return fabsf(x) < INFINITY; }
 
-// Exponent byte of a row whose largest finite magnitude is amax.
+// Exponent byte of a row whose largest finite magnitude is amax.  At most 119 + 127:
+// a scale meets softmax weights of up to 2^kTreeTau = 2^8, and 2^127 is the last power of two.
+// Magnitudes past 464 2^119 = 3.08e38 round past the last code, 448, to NaN, e4m3's
+// own conversion.
 __device__ __forceinline__ uint32_t q_exponent(float amax) {
     if (amax == 0.f) return 127;
     // amax = m 2^e, 1/2 <= m < 1: 448 = 7/8 2^9

@@ -20,6 +20,12 @@
 // fetch the rows again from the L2, and once their workgroups would be more than two
 // a CU tree_wide.hip's kernel takes them.
 //
+// The weights of bf16 and 8-bit rows are rounded to bf16 (2^-8 of a weight at most), as
+// the decode and the prefill round theirs: they are an operand of the bf16 products (fp32 ones
+// run at an eighth of their rate: 153 and 1225 TFLOP/s for 8192^3).  The denominators sum them
+// unrounded in fp32.  Measured against 64 bits: 0.0020 - 0.0023 of the output's norm,
+// of which the output's own rounding is 0.0017.  No weight of fp32 rows is rounded.
+//
 // The codes of an 8-bit cache become bf16 in registers, exactly, and a row's
 // power of two is put on its logit and on its softmax weight instead of its d
 // features: as exact, for one product a key.

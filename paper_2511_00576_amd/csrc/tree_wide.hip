@@ -8,6 +8,8 @@
 // TB/s; 25.5 without the arithmetic, 35.5 without the requests), e4m3, 64 x 8 heads
 // of 48 columns 28.8 us.
 //
+// Weights are rounded to bf16 for their products, their sums are fp32: see tree.hip.
+//
 // Blocks: summaries first, then the window, then the drafted tokens (32 rows,
 // bf16).  They are requested ahead by LDS DMA into a ring of stages.  A wave
 // holds 32 columns; S^T = K Q^T, then O^T += V^T P^T on 32x32x16 products.  With

@@ -521,7 +521,8 @@ def qk_norm_rope(x, H: int, Hkv: int, turns=None, q_weight=None, k_weight=None, 
     no norm).  `turns`: rope_turns' frequencies (None: no rotation).  The
     token's position is start[b] (int32 [B], a ragged cache's n_tok for one;
     None: 0) + offsets[b, l] (int32 [B, L]; None: l).  `out` = (Q, K, V)
-    preallocated."""
+    preallocated.  The outputs carry no autograd history:
+    qk_norm_rope_backward gives the gradients."""
     args, dev, B, L, d = _norm_rope_args(x, H, Hkv, turns, q_weight, k_weight, eps, start, offsets, interleaved)
     code = _dtype_code(x)
     if out is None:
@@ -569,8 +570,8 @@ class QuantCache:
     """Ragged decode cache of e4m3 rows with a power of two each (see
     eva_qcache in eva.h): k_ring [B, Hkv, R, d], vt_ring [B, Hkv, R // 16, d, 16],
     k_sum, vt_sum likewise over S_max, and each row's exponent byte in *_exp.
-    Queries, keys, values and outputs are bf16.  `max_tokens` bounds every
-    sequence."""
+    Queries, keys, values and outputs are bf16.  Entries that are not finite, or
+    above 3.08e38, are held as NaN.  `max_tokens` bounds every sequence."""
 
     dtype = torch.bfloat16  # of the rows outside
 
