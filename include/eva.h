@@ -32,6 +32,9 @@
  * Element types: EVA_BF16 (bfloat16 storage, fp32 accumulation; the softmax
  * weights are rounded to bf16 before the weighted sum of values) or EVA_F32
  * (fp32 throughout).  One call uses one type for every tensor it touches.
+ * Weighted sums of values are divided by the weights' sum at the end, and a
+ * weight is up to 2^8 before that: over n keys, values beyond 2^120 / n may
+ * overflow fp32.
  * Head dimension d must be 64 or 128.
  *
  * Streams and ownership: `stream` is a hipStream_t passed as void* (NULL =
