@@ -676,6 +676,141 @@ int eva_qtree_attention(const eva_qcache* cache, const void* q, const void* k, c
                         const int* n_nodes, void* o, int T, const int* active, void* ws, size_t ws_bytes, void* stream);
 size_t eva_qtree_workspace_bytes(const eva_qcache* cache, int T);
 
+/*
+ * Paged cache: the exact keys and values of layers that keep full softmax
+ * attention (the hybrid models, some of whose layers are not replaced), for
+ * sequences of any lengths.  A pool of n_pages pages of P tokens holds the rows of
+ * all of them; a table, which the layers share, says which pages a sequence has.
+ * Position p of sequence b lies in page table[b][p / P], place p mod P: its slot is
+ * that page times P plus the place.  (The prompt's own attention, and training,
+ * are eva_prefill's with W >= L.)
+ *
+ * The struct is caller-owned host memory, the arrays caller-owned device memory,
+ * int32.  The calls below read and advance the counts on the device, so that a step
+ * has no host-side state and can be captured in a graph and replayed; calls that
+ * change a table have to be ordered with the others on it.
+ *   n_tok       [B]             tokens held (start: 0)
+ *   table       [B][max_pages]  pages in their order; -1 where there is none (start: -1)
+ *   free_pages  [n_pages]       a stack of the pages that nobody has: the first
+ *   n_free      [1]             n_free of them (start: every page, n_pages)
+ * P is 16, 32, 64, 128 or 256.  Limits: n_pages P and max_pages P at most 2^30, B max_pages
+ * below 2^31, B and B H_kv at most 65535 (UNSUPPORTED).  Counts outside what a
+ * sequence has room for are read as the nearest one inside.  Two sequences may name the same
+ * pages (a common prompt) where the caller writes the table: eva_paged_decode and
+ * eva_paged_select read them, but eva_page_truncate gives back what each of them names.
+ */
+typedef struct eva_page_table {
+    int B;
+    int P;          /* tokens of a page */
+    int n_pages;    /* pages of the pool */
+    int max_pages;  /* pages that one sequence may have */
+    int* n_tok;
+    int* table;
+    int* free_pages;
+    int* n_free;
+} eva_page_table;
+
+/*
+ * Pages and slots for new tokens: sequence b asks for counts[b] of them (device int32
+ * [B], clamped to 0 .. T; NULL: T each).  With n = n_tok[b] and need_b = ceil((n +
+ * counts[b]) / P) - ceil(n / P) new pages,
+ *     granted[b] = counts[b]  if need_b = 0, or the needs of the sequences up to and
+ *                             with b are n_free pages together or less;
+ *                  0          else, and where n + counts[b] exceeds max_pages P (such
+ *                             a sequence needs nothing).
+ * (So a sequence that the free pages do not suffice for holds up later ones that
+ * need pages too: they do not overtake it.)  New pages are taken from the top of
+ * the stack in the order of (sequence, page) and entered in the table,
+ * n_tok[b] += granted[b], and
+ *     slots[b][i] = slot of the token at position n + i for i < granted[b], else -1
+ *     start[b]    = n, the position of the first one (eva_qk_norm_rope's `start`)
+ * slots [B][T], start, granted [B]: device int32.  Nothing else is changed.
+ * Errors: INVALID (malformed table, T < 1, null or misaligned pointers),
+ * UNSUPPORTED (sizes, T above 2^30).
+ */
+int eva_page_extend(const eva_page_table* table, const int* counts, int T, int* slots, int* start, int* granted,
+                    void* stream);
+
+/*
+ * Sequence b keeps its first lens[b] tokens (device int32 [B]; all of them where it
+ * has fewer, none where lens[b] < 0): rejected tokens are taken back, a finished
+ * sequence (0) leaves.  The pages that no token is left in go back on the stack, the
+ * last sequence's last page first, so that after an eva_page_extend whose tokens are
+ * taken back again table and stack are what they were; their entries become -1.
+ * Errors: as eva_page_extend.
+ */
+int eva_page_truncate(const eva_page_table* table, const int* lens, void* stream);
+
+/*
+ * The rows of one layer: caller-owned device memory, 16-byte aligned.
+ *   k       [n_pages][H_kv][P][d]
+ *   vt      [n_pages][H_kv][P / 8][d][8]  values in tiles of 8 places (as eva_cache)
+ *   k_mean  [n_pages][H_kv][d], fp32: the mean of a page's keys, kept for complete
+ *           pages; NULL where no pages are chosen
+ * P and n_pages are the table's; one table serves pools of any H, H_kv, d, dtype.
+ */
+typedef struct eva_pcache {
+    int H, H_kv, d;
+    int dtype;   /* eva_dtype */
+    int P;
+    int n_pages;
+    void* k;
+    void* vt;
+    float* k_mean;
+} eva_pcache;
+
+/*
+ * Write new tokens' rows into their slots: k_new, v_new [B][H_kv][T][d], slots
+ * device int32 [B][T] as eva_page_extend gives them (tokens of one sequence in successive
+ * places, then -1: those are not written, nor are slots outside the pool).  A page
+ * whose last place is written gets its mean key, from all its keys as the pool holds
+ * them, with the same bits however many calls filled it.  Where two sequences are
+ * given the same slot either row may stay.
+ * Errors: INVALID (malformed cache, sizes, null or misaligned pointers),
+ * UNSUPPORTED (d, dtype, T above 2^30, sizes).
+ */
+int eva_paged_append(const eva_pcache* cache, const void* k_new, const void* v_new, const int* slots, int B, int T,
+                     void* stream);
+
+/*
+ * Attention of one query a sequence over its tokens: q, o [B][H][d] in the cache's
+ * dtype,
+ *     o[b][h] = sum_m softmax_m(q . k_m / sqrt(d)) v_m
+ * over all positions m < n_tok[b] (the query is that of the last one, appended before), or,
+ * with pages (device int32 [B][H_kv][S], as eva_paged_select gives them; NULL: S =
+ * 0), over those in the first min(S, pages held) listed pages of the kv head, each as
+ * often as it stands there (entries that are none of the sequence's pages: nothing).
+ * A row without keys is zeros.  Rows of sequences that are not active (device int32 [B], 0; NULL: all are)
+ * are left as they were.  A row that meets an entry of the table outside the pool is NaN.
+ * ws: optional device scratch of eva_paged_decode_workspace_bytes() bytes, which
+ * every call that overlaps another needs for its own: the chunks of 32 tokens of all
+ * rows are shared evenly by the workgroups, and rows that several of them had are
+ * joined by a second launch; with less, a workgroup takes each row (and 16 heads).
+ * The same call gives the same bits; the order of a row's sum depends on all lengths.
+ * Errors: INVALID (malformed or different table and cache, null or misaligned
+ * pointers, S), UNSUPPORTED (d, dtype, sizes).
+ */
+int eva_paged_decode(const eva_pcache* cache, const eva_page_table* table, const void* q, void* o, const int* pages, int S,
+                     const int* active, void* ws, size_t ws_bytes, void* stream);
+size_t eva_paged_decode_workspace_bytes(const eva_pcache* cache, const eva_page_table* table, int S);
+
+/*
+ * The pages that the queries of each kv head choose: pages [B][H_kv][S] (device
+ * int32), ascending, then -1.  Of a sequence that has S pages or fewer: all of them;
+ * else its `first` first ones, its `last` last ones (the page that is being filled among them)
+ * and of the others those with the highest
+ *     score_j = max over the kv head's query heads of q . k_mean[page j]
+ * (64-bit sums; of equal scores the lower page's, a NaN above all).  q [B][H][d].
+ * 0 <= first, 1 <= last, first + last <= S.  The scores need a mean of every complete page.
+ * ws: device scratch of eva_paged_select_workspace_bytes() bytes (0: none needed);
+ * every byte the call reads it writes first.
+ * Errors: as eva_paged_decode; INVALID for a cache without k_mean, CAPACITY
+ * (workspace too small).
+ */
+int eva_paged_select(const eva_pcache* cache, const eva_page_table* table, const void* q, int S, int first, int last,
+                     int* pages, void* ws, size_t ws_bytes, void* stream);
+size_t eva_paged_select_workspace_bytes(const eva_pcache* cache, const eva_page_table* table, int S);
+
 /* Static description of an eva_status value. */
 const char* eva_status_string(int status);
 

@@ -62,6 +62,13 @@ SYMBOLS = (
     "eva_qappend_decode",
     "eva_qtree_attention",
     "eva_qtree_workspace_bytes",
+    "eva_page_extend",
+    "eva_page_truncate",
+    "eva_paged_append",
+    "eva_paged_decode",
+    "eva_paged_decode_workspace_bytes",
+    "eva_paged_select",
+    "eva_paged_select_workspace_bytes",
     "eva_status_string",
 )
 
@@ -99,6 +106,22 @@ class EvaQCacheStruct(ctypes.Structure):
         ("k_sum", ctypes.c_void_p), ("vt_sum", ctypes.c_void_p),
         ("k_ring_exp", ctypes.c_void_p), ("v_ring_exp", ctypes.c_void_p),
         ("k_sum_exp", ctypes.c_void_p), ("v_sum_exp", ctypes.c_void_p),
+    ]
+
+
+class EvaPageTableStruct(ctypes.Structure):
+    _fields_ = [
+        ("B", ctypes.c_int), ("P", ctypes.c_int), ("n_pages", ctypes.c_int), ("max_pages", ctypes.c_int),
+        ("n_tok", ctypes.c_void_p), ("table", ctypes.c_void_p), ("free_pages", ctypes.c_void_p),
+        ("n_free", ctypes.c_void_p),
+    ]
+
+
+class EvaPCacheStruct(ctypes.Structure):
+    _fields_ = [
+        ("H", ctypes.c_int), ("H_kv", ctypes.c_int), ("d", ctypes.c_int), ("dtype", ctypes.c_int),
+        ("P", ctypes.c_int), ("n_pages", ctypes.c_int),
+        ("k", ctypes.c_void_p), ("vt", ctypes.c_void_p), ("k_mean", ctypes.c_void_p),
     ]
 
 
@@ -195,6 +218,21 @@ def load():
     lib.eva_qdecode_workspace_bytes.argtypes = [qp]
     lib.eva_qappend_decode.restype = i
     lib.eva_qappend_decode.argtypes = [qp, vp, vp, vp, vp, vp, vp, sz, vp]
+    tp, pp = ctypes.POINTER(EvaPageTableStruct), ctypes.POINTER(EvaPCacheStruct)
+    lib.eva_page_extend.restype = i
+    lib.eva_page_extend.argtypes = [tp, vp, i, vp, vp, vp, vp]
+    lib.eva_page_truncate.restype = i
+    lib.eva_page_truncate.argtypes = [tp, vp, vp]
+    lib.eva_paged_append.restype = i
+    lib.eva_paged_append.argtypes = [pp, vp, vp, vp, i, i, vp]
+    lib.eva_paged_decode.restype = i
+    lib.eva_paged_decode.argtypes = [pp, tp, vp, vp, vp, i, vp, vp, sz, vp]
+    lib.eva_paged_decode_workspace_bytes.restype = sz
+    lib.eva_paged_decode_workspace_bytes.argtypes = [pp, tp, i]
+    lib.eva_paged_select.restype = i
+    lib.eva_paged_select.argtypes = [pp, tp, vp, i, i, i, vp, vp, sz, vp]
+    lib.eva_paged_select_workspace_bytes.restype = sz
+    lib.eva_paged_select_workspace_bytes.argtypes = [pp, tp, i]
     lib.eva_status_string.restype = ctypes.c_char_p
     lib.eva_status_string.argtypes = [i]
     _lib = lib

@@ -17,7 +17,7 @@ LIB = os.path.join(HERE, "libeva.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 SOURCES = ["summary.hip", "prefill.hip", "prefill_mfma.hip", "decode.hip", "backward.hip", "norm_rope.hip",
-           "qcache.hip", "tree.hip", "tree_wide.hip", "eva_api.cpp"]
+           "qcache.hip", "tree.hip", "tree_wide.hip", "pages.hip", "paged.hip", "paged_select.hip", "eva_api.cpp"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -28,7 +28,8 @@ FLAGS = [
 # Per-source code-generation options.  The decode kernels keep their matrix-core
 # accumulators in ordinary VGPRs: otherwise they live in AGPRs and every
 # chunk's online-softmax rescale copies all of them out and back.
-SOURCE_FLAGS = {src: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"] for src in ("decode.hip", "tree.hip", "tree_wide.hip")}
+SOURCE_FLAGS = {src: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"] for src in ("decode.hip", "tree.hip", "tree_wide.hip",
+                                                                          "paged.hip")}
 
 
 def _compile(src: str, verbose: bool) -> str:

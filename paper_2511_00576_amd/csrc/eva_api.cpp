@@ -10,6 +10,7 @@
 #include "../../include/eva.h"
 #include "eva_device.hpp"
 #include "eva_kernels.hpp"
+#include "paged.hpp"
 
 using eva::bf16;
 
@@ -1248,6 +1249,175 @@ int eva_qtree_attention(const eva_qcache* cache, const void* q, const void* k, c
                      q_chunks(cache) + (T + 31) / 32, ws, ws_bytes);
     if (st != EVA_OK) return st;
     return launch_q(p, cache->d, stream);
+}
+
+}  // extern "C"
+
+// ---- paged cache -----------------------------------------------------------------
+namespace {
+
+bool page_size(int P) { return P == 16 || P == 32 || P == 64 || P == 128 || P == 256; }
+
+int check_table(const eva_page_table* t) {
+    if (!t || t->B < 1 || !page_size(t->P) || t->n_pages < 1 || t->max_pages < 1) return EVA_ERR_INVALID;
+    const void* arrays[] = {t->n_tok, t->table, t->free_pages, t->n_free};
+    for (const void* p : arrays)
+        if (!p || !aligned4(p)) return EVA_ERR_INVALID;
+    // slots and positions stay below 2^30, entries of the table and workgroups in 32 bits
+    if (t->n_pages > kMaxLen / t->P || t->max_pages > kMaxLen / t->P || t->B > 65535 ||
+        (long long)t->B * t->max_pages > 0x7fffffffLL)
+        return EVA_ERR_UNSUPPORTED;
+    return EVA_OK;
+}
+
+int check_pool(const eva_pcache* c) {
+    if (!c || c->H < 1 || c->H_kv < 1 || c->H % c->H_kv != 0 || !page_size(c->P) || c->n_pages < 1) return EVA_ERR_INVALID;
+    const int st = supported(c->d, c->dtype);
+    if (st != EVA_OK) return st;
+    if (!c->k || !c->vt || !aligned16(c->k) || !aligned16(c->vt) || !aligned16(c->k_mean)) return EVA_ERR_INVALID;
+    if (c->n_pages > kMaxLen / c->P || c->H_kv > 65535) return EVA_ERR_UNSUPPORTED;
+    return EVA_OK;
+}
+
+// A pool and the table that gives out its pages.
+int check_paged(const eva_pcache* c, const eva_page_table* t) {
+    int st = check_pool(c);
+    if (st != EVA_OK) return st;
+    st = check_table(t);
+    if (st != EVA_OK) return st;
+    if (c->P != t->P || c->n_pages != t->n_pages) return EVA_ERR_INVALID;
+    if ((long long)t->B * c->H_kv > 65535) return EVA_ERR_UNSUPPORTED;
+    return EVA_OK;
+}
+
+int page_shift(int P) { return __builtin_ctz((unsigned)P); }
+
+eva::PageTableView table_of(const eva_page_table* t) {
+    return eva::PageTableView{t->B, page_shift(t->P), t->n_pages, t->max_pages, t->n_tok, t->table, t->free_pages, t->n_free};
+}
+
+// Rows of a decode and the workgroups that share them; one per row where no row
+// has more chunks than a workgroup takes anyway.
+struct PagedRoute {
+    long long rows, wgs;  // wgs = 0: one per row
+    int n_hg;
+};
+int paged_route(PagedRoute& r, const eva_pcache* c, const eva_page_table* t, int S) {
+    r.n_hg = (c->H / c->H_kv + 15) / 16;
+    r.rows = (long long)t->B * c->H_kv * r.n_hg;
+    const long long pages = S > 0 && S < t->max_pages ? S : t->max_pages;
+    const long long chunks = pages * t->P <= 32 ? 1 : pages * t->P / 32 + (pages * t->P % 32 != 0);
+    if (r.rows * chunks > 0x7fffffffLL || r.rows > 0x7fffff) return EVA_ERR_UNSUPPORTED;
+    r.wgs = 0;
+    if (chunks > eva::kPagedMinPart) {
+        const long long parts = (r.rows * chunks + eva::kPagedMinPart - 1) / eva::kPagedMinPart;
+        r.wgs = parts < eva::kPagedWgs ? parts : eva::kPagedWgs;
+    }
+    return EVA_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int eva_page_truncate(const eva_page_table* table, const int* lens, void* stream) {
+    const int st = check_table(table);
+    if (st != EVA_OK) return st;
+    if (!lens || !aligned4(lens)) return EVA_ERR_INVALID;
+    return hip_status(eva::launch_page_truncate(table_of(table), lens, static_cast<hipStream_t>(stream)));
+}
+
+int eva_page_extend(const eva_page_table* table, const int* counts, int T, int* slots, int* start, int* granted,
+                    void* stream) {
+    const int st = check_table(table);
+    if (st != EVA_OK) return st;
+    if (T < 1 || !slots || !start || !granted || !aligned4(counts) || !aligned4(slots) || !aligned4(start) ||
+        !aligned4(granted))
+        return EVA_ERR_INVALID;
+    if (T > kMaxLen) return EVA_ERR_UNSUPPORTED;
+    return hip_status(eva::launch_page_extend(table_of(table), counts, T, slots, start, granted,
+                                              static_cast<hipStream_t>(stream)));
+}
+
+int eva_paged_append(const eva_pcache* cache, const void* k_new, const void* v_new, const int* slots, int B, int T,
+                     void* stream) {
+    const int st = check_pool(cache);
+    if (st != EVA_OK) return st;
+    if (B < 1 || T < 1 || !k_new || !v_new || !slots || !aligned16(k_new) || !aligned16(v_new) || !aligned4(slots))
+        return EVA_ERR_INVALID;
+    if (T > kMaxLen || B > 65535) return EVA_ERR_UNSUPPORTED;
+    const eva::PagedAppendParams p{cache->k, cache->vt, cache->k_mean, k_new, v_new, slots, B, cache->H_kv, T,
+                                   page_shift(cache->P), cache->n_pages};
+    // threads of the launch stay below 2^32
+    if ((long long)((T + 2LL * cache->P - 2) / cache->P) * B * cache->H_kv > 0xffffff) return EVA_ERR_UNSUPPORTED;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return hip_status(dispatch(cache->d, cache->dtype, [&](auto dd, auto t) {
+        return eva::launch_paged_append<decltype(dd)::value, decltype(t)>(p, s);
+    }));
+}
+
+size_t eva_paged_select_workspace_bytes(const eva_pcache* cache, const eva_page_table* table, int S) {
+    if (check_paged(cache, table) != EVA_OK || S < 1 || S >= table->max_pages) return 0;
+    return (size_t)table->B * cache->H_kv * table->max_pages * sizeof(unsigned long long);
+}
+
+int eva_paged_select(const eva_pcache* cache, const eva_page_table* table, const void* q, int S, int first, int last,
+                     int* pages, void* ws, size_t ws_bytes, void* stream) {
+    const int st = check_paged(cache, table);
+    if (st != EVA_OK) return st;
+    if (S < 1 || first < 0 || last < 1 || (long long)first + last > S || !q || !pages || !cache->k_mean || !aligned16(q) ||
+        !aligned4(pages))
+        return EVA_ERR_INVALID;
+    const size_t need = eva_paged_select_workspace_bytes(cache, table, S);
+    if (need && (!ws || !aligned16(ws))) return EVA_ERR_INVALID;
+    if (ws_bytes < need) return EVA_ERR_CAPACITY;
+    const eva::SelectParams p{table_of(table), cache->k_mean, q, pages, static_cast<unsigned long long*>(ws), S, first, last,
+                              cache->H, cache->H_kv, cache->H / cache->H_kv};
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return hip_status(dispatch(cache->d, cache->dtype, [&](auto dd, auto t) {
+        return eva::launch_paged_select<decltype(dd)::value, decltype(t)>(p, s);
+    }));
+}
+
+size_t eva_paged_decode_workspace_bytes(const eva_pcache* cache, const eva_page_table* table, int S) {
+    PagedRoute r;
+    if (check_paged(cache, table) != EVA_OK || S < 0 || paged_route(r, cache, table, S) != EVA_OK || r.wgs == 0) return 0;
+    return eva::paged_ws_bytes(r.rows, r.wgs, cache->d);
+}
+
+int eva_paged_decode(const eva_pcache* cache, const eva_page_table* table, const void* q, void* o, const int* pages, int S,
+                     const int* active, void* ws, size_t ws_bytes, void* stream) {
+    int st = check_paged(cache, table);
+    if (st != EVA_OK) return st;
+    if (!q || !o || !aligned16(q) || !aligned16(o) || (pages ? S < 1 : S != 0) || !aligned4(pages) || !aligned4(active))
+        return EVA_ERR_INVALID;
+    PagedRoute r;
+    st = paged_route(r, cache, table, S);
+    if (st != EVA_OK) return st;
+    eva::PagedParams p{};
+    p.t = table_of(table);
+    p.k = cache->k;
+    p.vt = cache->vt;
+    p.pages = pages;
+    p.active = active;
+    p.q = q;
+    p.o = o;
+    p.S = S;
+    p.H = cache->H;
+    p.Hkv = cache->H_kv;
+    p.G = cache->H / cache->H_kv;
+    p.n_hg = r.n_hg;
+    p.rows = (int)r.rows;
+    p.wgs = (int)r.wgs;
+    p.f_unit = eva::FastDiv(cache->H_kv * r.n_hg);
+    p.f_hg = eva::FastDiv(r.n_hg);
+    p.scale_log2 = (float)(1.4426950408889634 / sqrt((double)cache->d));
+    if (r.wgs > 0 && ws && aligned16(ws) && ws_bytes >= eva::paged_ws_bytes(r.rows, r.wgs, cache->d))
+        p.ws = static_cast<float*>(ws);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return hip_status(dispatch(cache->d, cache->dtype, [&](auto dd, auto t) {
+        return eva::launch_paged_decode<decltype(dd)::value, decltype(t)>(p, s);
+    }));
 }
 
 }  // extern "C"

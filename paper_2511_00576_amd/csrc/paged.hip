@@ -1,0 +1,532 @@
+// Decode over a paged cache: one query per sequence attends all its tokens, or
+// those of a list of pages.
+//
+// A row is (sequence, kv head, group of up to 16 query heads); its keys go by
+// chunks of 32 tokens, each two halves of 16 that lie in one page each.  Per
+// chunk a wave computes S^T = K Q^T and O^T += V^T P^T on the matrix cores with
+// the operands read straight from memory, 16 bytes a lane, the softmax's maximum
+// and sum running: every key and value is read once for the heads that share it.
+//
+// The batch's rows may differ in length by any factor, and their lengths are on
+// the device.  So the launch has a fixed number of workgroups, and they share the
+// chunks of all rows, one row after the other, in equal contiguous parts: a
+// workgroup finds its part from the sequences' token counts (a scan, a microsecond),
+// and rows that lie in more than one part are joined by a second launch.
+#include "paged.hpp"
+
+namespace eva {
+
+namespace {
+
+constexpr float kPagedTau = 8.f;  // log2 units: unscaled weights stay <= 256
+constexpr int kPagedWaves = 4;
+
+// Pages that a row's query attends, of a sequence of n tokens: all it has, or the
+// first so many of its list.
+__device__ __forceinline__ int row_pages(const PagedParams& a, int n) {
+    const int held = pages_of(n, a.t.shift);
+    return a.pages ? min(a.S, held) : held;
+}
+// Chunks of a row; at least one, which writes the zeros of a sequence without tokens;
+// none for an inactive one.
+__device__ __forceinline__ int row_chunks(const PagedParams& a, int b) {
+    if (a.active && a.active[b] == 0) return 0;
+    const int n = held_tokens(a.t, b);
+    const int len = a.pages ? row_pages(a, n) << a.t.shift : n;
+    return max((len + 31) >> 5, 1);
+}
+
+__device__ __forceinline__ int wave_sum(int x) {
+#pragma unroll
+    for (int i = 32; i; i >>= 1) x += __shfl_xor(x, i);
+    return x;
+}
+
+// A word that every lane wants and that nothing writes during the launch: through the
+// scalar cache, so that waiting for it does not wait for the vector loads before it.
+__device__ __forceinline__ int scalar_load(const int* p) {
+    return *(const __attribute__((address_space(4))) int*)p;
+}
+
+// 16 tokens of a page.
+struct Half {
+    size_t at;  // elements from the pool's start to their rows (keys and values alike)
+    int valid;  // of them, the first so many are attended
+    bool lost;  // the table names no page of the pool
+};
+
+// Half h of chunk ch of the row (b, kvh).
+template <int D>
+__device__ __forceinline__ Half locate(const PagedParams& a, int b, int kvh, int n, int n_pages, int ch, int h) {
+    const int shift = a.t.shift;
+    const int v = ch * 32 + h * 16, e = v >> shift, off = v & ((1 << shift) - 1);
+    Half r{0, 0, false};
+    if (e < n_pages) {
+        int lp = e;
+        if (a.pages) lp = scalar_load(a.pages + ((size_t)b * a.Hkv + kvh) * a.S + e);
+        const int left = n - ((lp << shift) + off);
+        if ((unsigned)lp < (unsigned)pages_of(n, shift) && left > 0) {
+            const int page = scalar_load(a.t.table + (size_t)b * a.t.max_pages + lp);
+            r.valid = min(left, 16);
+            r.lost = (unsigned)page >= (unsigned)a.t.n_pages;
+            r.at = (((size_t)(r.lost ? 0 : page) * a.Hkv + kvh) << shift) * D + (size_t)off * D;
+        }
+    }
+    return r;
+}
+
+// The running state of a wave: 16 columns, per lane (g, c16) the features
+// 16 db + 4 g .. + 3 of column c16.
+template <int D>
+struct RowState {
+    float m, l;
+    floatx4 acc[D / 16];
+    __device__ __forceinline__ void clear() {
+        m = -INFINITY;
+        l = 0.f;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) acc[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+    // Scores of a chunk (two blocks of four per lane) become weights; the reference
+    // maximum moves only when the chunk's exceeds it by more than kPagedTau.
+    __device__ __forceinline__ void weigh(floatx4 (&s)[2], float scale) {
+        float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
+                         fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+        mx = xgroup_max(mx) * scale;
+        const bool raise = mx > m + kPagedTau;
+        if (__builtin_amdgcn_ballot_w64(raise)) {
+            const float next = raise ? mx : m;
+            const float alpha = raise ? fast_exp2(m - next) : 1.f;  // the first time: exp2(-inf) = 0
+            l *= alpha;
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) acc[i] *= alpha;
+            m = next;
+        }
+        // no maximum yet (scores of -inf alone): their weights are 0
+        const float off = m == -INFINITY ? 0.f : -m;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                s[kb][i] = fast_exp2(fmaf(s[kb][i], scale, off));
+                l += s[kb][i];
+            }
+    }
+};
+
+// Query fragments, and one chunk's products, by type.  `valid` has a bit for each
+// of the chunk's tokens that is attended, `lost` for each whose page there is not.
+template <int D, typename T>
+struct Chunk;
+
+template <int D>
+struct Chunk<D, bf16> {
+    bf16x8 k[2][D / 32], v[D / 16];
+    // Rows are permuted so that the eight scores of a lane are keys 8g .. 8g + 7 (block kb:
+    // + 4 kb + i), the slots of its 16 bytes of a feature's values.
+    static __device__ __forceinline__ void query(bf16x8 (&q)[D / 32], const bf16* row, int g) {
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) q[i] = *reinterpret_cast<const bf16x8*>(row + 32 * i + 8 * g);
+    }
+    static __device__ __forceinline__ int mask_of(uint32_t bits, int g, int kb) { return (int)(bits >> (8 * g + 4 * kb)) & 15; }
+    __device__ __forceinline__ void load(const bf16* kp, const bf16* vp, size_t at0, size_t at1, int g, int c) {
+        const bf16* kr = kp + (c >= 8 ? at1 : at0) + ((c >> 2 & 1) * 8 + (c & 3)) * D + 8 * g;
+        const bf16* vr = vp + (g >= 2 ? at1 : at0) + vt_index<D>(c, 8 * (g & 1));
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i)
+                k[kb][i] = __builtin_nontemporal_load(reinterpret_cast<const bf16x8*>(kr + 4 * kb * D + 32 * i));
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i)
+            v[i] = __builtin_nontemporal_load(reinterpret_cast<const bf16x8*>(vr + 16 * i * kVtTile));
+    }
+    __device__ __forceinline__ void scores(const bf16x8 (&q)[D / 32], floatx4 (&s)[2]) const {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            s[kb] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) s[kb] = mfma_bf16(k[kb][i], q[i], s[kb]);
+        }
+    }
+    // values of tokens that are not attended may be any bits: they become zeros
+    __device__ __forceinline__ void keep_values(uint32_t valid, int g) {
+        uint32_t keep[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t two = valid >> (8 * g + 2 * i);
+            keep[i] = (two & 1 ? 0x0000ffffu : 0u) | (two & 2 ? 0xffff0000u : 0u);
+        }
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) {
+            u32x4 w = __builtin_bit_cast(u32x4, v[i]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] &= keep[j];
+            v[i] = __builtin_bit_cast(bf16x8, w);
+        }
+    }
+    // The weights are rounded to bf16, the products' operand (fp32 products run at an
+    // eighth of the rate); the denominator sums them unrounded.
+    __device__ __forceinline__ void add(const floatx4 (&p)[2], floatx4 (&acc)[D / 16]) const {
+        bf16x8 pf;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) pf[i] = to_bf16(p[i / 4][i % 4]);
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) acc[i] = mfma_bf16(v[i], pf, acc[i]);
+    }
+};
+
+template <int D>
+struct Chunk<D, float> {
+    floatx4 k[2][D / 16], v[2][D / 16];
+    // Contraction step (i, e) of the scores: feature 16 i + 4 g + e; of the values: key
+    // 16 kb + 4 g + e, whose weight the lane holds already.
+    static __device__ __forceinline__ void query(floatx4 (&q)[D / 16], const float* row, int g) {
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) q[i] = *reinterpret_cast<const floatx4*>(row + 16 * i + 4 * g);
+    }
+    static __device__ __forceinline__ int mask_of(uint32_t bits, int g, int kb) { return (int)(bits >> (16 * kb + 4 * g)) & 15; }
+    __device__ __forceinline__ void load(const float* kp, const float* vp, size_t at0, size_t at1, int g, int c) {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            const float* kr = kp + (kb ? at1 : at0) + c * D + 4 * g;
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i)
+                k[kb][i] = __builtin_nontemporal_load(reinterpret_cast<const floatx4*>(kr + 16 * i));
+        }
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            const float* vr = vp + (kb ? at1 : at0) + vt_index<D>(c, 4 * g);
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i)
+                v[kb][i] = __builtin_nontemporal_load(reinterpret_cast<const floatx4*>(vr + 16 * i * kVtTile));
+        }
+    }
+    __device__ __forceinline__ void scores(const floatx4 (&q)[D / 16], floatx4 (&s)[2]) const {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            s[kb] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[kb] = mfma_f32(k[kb][i][e], q[i][e], s[kb]);
+        }
+    }
+    __device__ __forceinline__ void keep_values(uint32_t valid, int g) {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            const int m = mask_of(valid, g, kb);
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[kb][i][e] = m >> e & 1 ? v[kb][i][e] : 0.f;
+        }
+    }
+    __device__ __forceinline__ void add(const floatx4 (&p)[2], floatx4 (&acc)[D / 16]) const {
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[i] = mfma_f32(v[kb][i][e], p[kb][e], acc[i]);
+    }
+};
+
+template <typename T>
+struct QueryFragment;
+template <>
+struct QueryFragment<bf16> {
+    typedef bf16x8 type;
+    static constexpr int kFeatures = 32;
+};
+template <>
+struct QueryFragment<float> {
+    typedef floatx4 type;
+    static constexpr int kFeatures = 16;
+};
+
+__device__ __forceinline__ void store4(bf16* o, const floatx4& x) {
+    *reinterpret_cast<u32x2*>(o) = u32x2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
+}
+__device__ __forceinline__ void store4(float* o, const floatx4& x) { *reinterpret_cast<floatx4*>(o) = x; }
+
+// What a row's sums come to.  m = -inf: no key had a score above -inf; l tells
+// why: 0 no keys (zeros), else the formula has no value (-1: scores of -inf alone,
+// NaN: of NaN).
+__device__ __forceinline__ floatx4 finish(float m, float l, const floatx4& o) {
+    if (m == -INFINITY) {
+        const float x = l == 0.f ? 0.f : NAN;
+        return floatx4{x, x, x, x};
+    }
+    return o * (1.f / l);
+}
+
+// Workspace: an int2 for each row (x: -1, or 2 w + s for a row whose first part is share
+// s of workgroup w; y: how many workgroups after w hold the rest), then [wgs][2] shares
+// of [16] maxima, [16] sums, [16][D] weighted values.  Share 0 is that of a part's first row,
+// share 1 that of its last one.
+template <int D>
+__host__ __device__ constexpr int share_floats() { return 16 * (D + 2); }
+__device__ __forceinline__ float* shares_of(const PagedParams& a) { return a.ws + (a.rows + 1) / 2 * 4; }
+
+template <int D, typename T>
+__global__ __launch_bounds__(kPagedWaves * 64) void paged_decode_kernel(PagedParams a) {
+    constexpr int NW = kPagedWaves;
+    constexpr int COL = D + 4;  // 16 columns on distinct banks
+    typedef typename QueryFragment<T>::type Frag;
+    constexpr int NQ = D / QueryFragment<T>::kFeatures;
+    __shared__ float red_m[NW][16], red_l[NW][16];
+    __shared__ __attribute__((aligned(16))) float red_o[NW][16][COL];
+
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int g = lane >> 4, c16 = lane & 15;
+    const int unit = a.f_unit;  // rows of a sequence
+    const T* kp = static_cast<const T*>(a.k);
+    const T* vp = static_cast<const T*>(a.vt);
+
+    // this workgroup's chunks: `todo` from chunk c0 of row `row` of sequence b on
+    int b, row, c0, todo, part = 0;
+    if (a.ws) {
+        int total = 0;
+        for (int i = 0; i < a.t.B; i += 64) total += i + lane < a.t.B ? row_chunks(a, i + lane) : 0;
+        total = wave_sum(total) * unit;
+        part = max((total + a.wgs - 1) / a.wgs, kPagedMinPart);
+        const int from = (int)blockIdx.x * part;
+        if (from >= total) return;
+        todo = min(part, total - from);
+        // the sequence that holds chunk `from`
+        int before = 0, at = 0;
+        for (int i = 0;; i += 64) {
+            const int mine = i + lane < a.t.B ? row_chunks(a, i + lane) * unit : 0;
+            int upto = mine;
+#pragma unroll
+            for (int s = 1; s < 64; s <<= 1) {
+                const int y = __shfl_up(upto, s);
+                if (lane >= s) upto += y;
+            }
+            upto += before;
+            const unsigned long long past = __builtin_amdgcn_ballot_w64(upto > from);
+            if (past) {
+                const int l = __builtin_ctzll(past);
+                b = i + l;
+                at = from - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(mine, l));
+                break;
+            }
+            before = __builtin_amdgcn_readlane(upto, 63);
+        }
+        const int chunks = row_chunks(a, b);
+        row = at / chunks;
+        c0 = at - row * chunks;
+    } else {
+        b = (int)blockIdx.x / a.f_unit;
+        row = (int)blockIdx.x % a.f_unit;
+        c0 = 0;
+        todo = row_chunks(a, b);
+        if (todo == 0) return;
+    }
+    b = __builtin_amdgcn_readfirstlane(b);
+    row = __builtin_amdgcn_readfirstlane(row);
+    c0 = __builtin_amdgcn_readfirstlane(c0);
+    todo = __builtin_amdgcn_readfirstlane(todo);
+
+    for (bool first = true;; first = false) {
+        const int n = __builtin_amdgcn_readfirstlane(held_tokens(a.t, b));
+        const int n_pages = row_pages(a, n);
+        const int chunks = __builtin_amdgcn_readfirstlane(row_chunks(a, b));
+        const int c1 = min(chunks, c0 + todo);
+        const int kvh = row / a.f_hg, hg = row % a.f_hg;
+        const int h0 = kvh * a.G + hg * 16;
+        const int ncols = min(16, a.G - hg * 16);
+        // columns past ncols repeat the last head; their outputs are not stored
+        Frag q[NQ];
+        Chunk<D, T>::query(q, static_cast<const T*>(a.q) + ((size_t)b * a.H + h0 + min(c16, ncols - 1)) * D, g);
+
+        RowState<D> st;
+        st.clear();
+        bool any = false;
+        int ch = c0 + wave;
+        Half x0{0, 0, false}, x1{0, 0, false};
+        if (ch < c1) {
+            x0 = locate<D>(a, b, kvh, n, n_pages, ch, 0);
+            x1 = locate<D>(a, b, kvh, n, n_pages, ch, 1);
+        }
+        while (ch < c1) {
+            Chunk<D, T> x;
+            x.load(kp, vp, x0.at, x1.at, g, c16);
+            const uint32_t valid = (x0.valid ? 0xffffu >> (16 - x0.valid) : 0u) |
+                                   (x1.valid ? 0xffff0000u >> (16 - x1.valid) & 0xffff0000u : 0u);
+            const bool lost0 = x0.lost, lost1 = x1.lost;
+            ch += NW;
+            if (ch < c1) {
+                x0 = locate<D>(a, b, kvh, n, n_pages, ch, 0);
+                x1 = locate<D>(a, b, kvh, n, n_pages, ch, 1);
+            }
+            if (valid == 0) continue;
+            any = true;
+            floatx4 s[2];
+            x.scores(q, s);
+            if (valid != 0xffffffffu || lost0 || lost1) {
+                const uint32_t lost = (lost0 ? 0xffffu : 0u) | (lost1 ? 0xffff0000u : 0u);
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb) {
+                    const int in = Chunk<D, T>::mask_of(valid, g, kb), no = Chunk<D, T>::mask_of(lost, g, kb);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[kb][i] = in >> i & 1 ? no >> i & 1 ? NAN : s[kb][i] : -INFINITY;
+                }
+                x.keep_values(valid, g);
+            }
+            st.weigh(s, a.scale_log2);
+            x.add(s, st.acc);
+        }
+
+        // ---- the waves' parts of the row ----
+        float l = xgroup_sum(st.l);
+        if (any && st.m == -INFINITY && l == 0.f) l = -1.f;  // see finish()
+        if (g == 0) {
+            red_m[wave][c16] = st.m;
+            red_l[wave][c16] = l;
+        }
+        if (c16 < ncols) {
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) *reinterpret_cast<floatx4*>(&red_o[wave][c16][16 * i + 4 * g]) = st.acc[i];
+        }
+        __syncthreads();
+        const bool whole = c0 == 0 && c1 == chunks;
+        const int share = first ? 0 : 1;
+        float* part_ws = a.ws ? shares_of(a) + ((size_t)blockIdx.x * 2 + share) * share_floats<D>() : nullptr;
+        for (int t = tid; t < ncols * (D / 4); t += NW * 64) {
+            const int col = t / (D / 4), f = t % (D / 4) * 4;
+            float m = -INFINITY, sum = 0.f;
+            floatx4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < NW; ++w) m = fmaxf(m, red_m[w][col]);
+#pragma unroll
+            for (int w = 0; w < NW; ++w) {
+                // without a maximum there is no weight; sums of NaN stay, and where there is none at
+                // all the waves' reasons are summed as they are
+                const float mw = red_m[w][col];
+                const float wt = m == -INFINITY ? 1.f : mw == -INFINITY ? 0.f : fast_exp2(mw - m);
+                sum += wt * red_l[w][col];
+                o += wt * *reinterpret_cast<const floatx4*>(&red_o[w][col][f]);
+            }
+            if (whole) {
+                store4(static_cast<T*>(a.o) + ((size_t)b * a.H + h0 + col) * D + f, finish(m, sum, o));
+            } else {
+                if (f == 0) {
+                    part_ws[col] = m;
+                    part_ws[16 + col] = sum;
+                }
+                *reinterpret_cast<floatx4*>(part_ws + 32 + col * D + f) = o;
+            }
+        }
+        if (!a.ws) return;
+        if (c0 == 0 && tid == 0) {
+            int2 info = {-1, 0};
+            if (!whole) info = int2{2 * (int)blockIdx.x + share, (chunks - c1 + part - 1) / part};
+            reinterpret_cast<int2*>(a.ws)[b * unit + row] = info;
+        }
+        todo -= c1 - c0;
+        if (todo == 0) return;
+        c0 = 0;
+        if (++row == unit) {
+            row = 0;
+            do ++b;  // todo > 0: there is one
+            while (row_chunks(a, b) == 0);
+            b = __builtin_amdgcn_readfirstlane(b);
+        }
+        __syncthreads();  // the parts have been read
+    }
+}
+
+// Joins the shares of rows that more than one workgroup held: a workgroup per row,
+// threads over (share, column, four features), then over LDS.
+constexpr int kJoinThreads = 512;
+template <int D, typename T>
+__global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedParams a) {
+    __shared__ float red_m[kJoinThreads], red_l[kJoinThreads];
+    __shared__ __attribute__((aligned(16))) floatx4 red_o[kJoinThreads];
+    const int row = blockIdx.x;
+    const int b = row / a.f_unit;
+    if (row_chunks(a, b) == 0) return;  // inactive
+    const int2 info = reinterpret_cast<const int2*>(a.ws)[row];
+    if (info.x < 0) return;
+    const int kvh = row % a.f_unit / a.f_hg, hg = row % a.f_unit % a.f_hg;
+    const int ncols = min(16, a.G - hg * 16);
+    const int shares = 1 + info.y;
+    const float* first = shares_of(a) + (size_t)info.x * share_floats<D>();
+    const float* rest = shares_of(a) + (size_t)((info.x >> 1) + 1) * 2 * share_floats<D>();
+    const int items = ncols * (D / 4);  // 16 .. 512
+    const int groups = kJoinThreads / items;
+    const int grp = threadIdx.x / items, e = threadIdx.x % items;
+    const int col = e / (D / 4), f = e % (D / 4) * 4;
+    float M = -INFINITY, L = 0.f;
+    floatx4 O = {0.f, 0.f, 0.f, 0.f};
+    // NB shares' loads in flight together
+    constexpr int NB = 4;
+    if (grp < groups) {
+        for (int s0 = grp; s0 < shares; s0 += groups * NB) {
+            float m[NB], l[NB];
+            floatx4 o[NB];
+#pragma unroll
+            for (int i = 0; i < NB; ++i) {
+                const int s = min(s0 + i * groups, shares - 1);
+                const float* w = s == 0 ? first : rest + (size_t)(s - 1) * 2 * share_floats<D>();
+                m[i] = w[col];
+                l[i] = w[16 + col];
+                o[i] = *reinterpret_cast<const floatx4*>(w + 32 + col * D + f);
+            }
+            float top = M;
+#pragma unroll
+            for (int i = 0; i < NB; ++i) {
+                if (s0 + i * groups >= shares) {  // past the last
+                    m[i] = -INFINITY;
+                    l[i] = 0.f;
+                    o[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+                }
+                top = fmaxf(top, m[i]);
+            }
+            const float keep = top == -INFINITY ? 1.f : M == -INFINITY ? 0.f : fast_exp2(M - top);
+            L *= keep;
+            O *= keep;
+#pragma unroll
+            for (int i = 0; i < NB; ++i) {
+                const float wt = top == -INFINITY ? 1.f : m[i] == -INFINITY ? 0.f : fast_exp2(m[i] - top);
+                L += wt * l[i];
+                O += wt * o[i];
+            }
+            M = top;
+        }
+    }
+    red_m[threadIdx.x] = M;
+    red_l[threadIdx.x] = L;
+    red_o[threadIdx.x] = O;
+    __syncthreads();
+    if (grp != 0) return;
+    float top = M;
+    for (int i = 1; i < groups; ++i) top = fmaxf(top, red_m[i * items + e]);
+    float sum = 0.f;
+    floatx4 out = {0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < groups; ++i) {
+        const float m = red_m[i * items + e];
+        const float wt = top == -INFINITY ? 1.f : m == -INFINITY ? 0.f : fast_exp2(m - top);
+        sum += wt * red_l[i * items + e];
+        out += wt * red_o[i * items + e];
+    }
+    store4(static_cast<T*>(a.o) + ((size_t)b * a.H + kvh * a.G + hg * 16 + col) * D + f, finish(top, sum, out));
+}
+
+}  // namespace
+
+template <int D, typename T>
+hipError_t launch_paged_decode(const PagedParams& p, hipStream_t stream) {
+    paged_decode_kernel<D, T><<<p.ws ? p.wgs : p.rows, kPagedWaves * 64, 0, stream>>>(p);
+    if (p.ws) paged_join_kernel<D, T><<<p.rows, kJoinThreads, 0, stream>>>(p);
+    return hipGetLastError();
+}
+template hipError_t launch_paged_decode<64, bf16>(const PagedParams&, hipStream_t);
+template hipError_t launch_paged_decode<128, bf16>(const PagedParams&, hipStream_t);
+template hipError_t launch_paged_decode<64, float>(const PagedParams&, hipStream_t);
+template hipError_t launch_paged_decode<128, float>(const PagedParams&, hipStream_t);
+
+}  // namespace eva

@@ -1,0 +1,86 @@
+// Paged cache: parameters and launches of pages.hip (table, append), paged.hip
+// (decode) and paged_select.hip (choice of pages).
+//
+// A pool of n_pages pages of P = 2^shift tokens holds the rows of every sequence:
+// keys k [n_pages][Hkv][P][d], values vt [n_pages][Hkv][P / 8][d][8] (the decode
+// cache's 8-slot tiles: vt_index), mean keys [n_pages][Hkv][d] in fp32.  Position p
+// of sequence b lies in page table[b][p / P], place p mod P.
+#pragma once
+
+#include "eva_device.hpp"
+#include "eva_kernels.hpp"
+
+namespace eva {
+
+struct PageTableView {
+    int B, shift, n_pages, max_pages;
+    int* n_tok;   // [B]
+    int* table;   // [B][max_pages], -1: no page
+    int* free_pages;  // [n_pages], a stack of n_free[0] pages
+    int* n_free;
+};
+
+// Token counts are only ever used within what the table's row has room for.
+__device__ __forceinline__ int held_tokens(const PageTableView& t, int b) {
+    return min(max(t.n_tok[b], 0), t.max_pages << t.shift);
+}
+__host__ __device__ __forceinline__ int pages_of(int tokens, int shift) {
+    return (int)(((unsigned)tokens + (1u << shift) - 1) >> shift);
+}
+
+hipError_t launch_page_truncate(const PageTableView& t, const int* lens, hipStream_t stream);
+// slots [B][T], start [B], granted [B]
+hipError_t launch_page_extend(const PageTableView& t, const int* counts, int T, int* slots, int* start, int* granted,
+                              hipStream_t stream);
+
+struct PagedAppendParams {
+    void* k;
+    void* vt;
+    float* mean;       // or nullptr
+    const void* k_new; // [B][Hkv][T][d]
+    const void* v_new;
+    const int* slots;  // [B][T]
+    int B, Hkv, T, shift, n_pages;
+};
+template <int D, typename T>
+hipError_t launch_paged_append(const PagedAppendParams& p, hipStream_t stream);
+
+struct PagedParams {
+    PageTableView t;
+    const void* k;
+    const void* vt;
+    const int* pages;   // [B][Hkv][S] pages that a kv head's queries attend, or nullptr: all
+    const int* active;  // [B] or nullptr
+    const void* q;      // [B][H][d]
+    void* o;
+    float* ws;          // partials of split rows, nullptr: a workgroup per row
+    int S, H, Hkv, G;
+    int n_hg;           // groups of 16 query heads of a kv head
+    int rows;           // B Hkv n_hg
+    int wgs;            // workgroups that share all rows' chunks (with ws)
+    FastDiv f_unit, f_hg;  // divisors of Hkv n_hg and of n_hg
+    float scale_log2;
+};
+// The fewest chunks a workgroup takes: one for each of its four waves.
+constexpr int kPagedMinPart = 4;
+// Workgroups that share a decode's chunks: as many as the CUs hold at once.
+constexpr int kPagedWgs = 768;
+// Bytes of the workspace: a pair of ints per row, then two shares per workgroup.
+inline size_t paged_ws_bytes(long long rows, long long wgs, int d) {
+    return ((size_t)(rows + 1) / 2 * 4 + (size_t)wgs * 2 * 16 * (d + 2)) * sizeof(float);
+}
+template <int D, typename T>
+hipError_t launch_paged_decode(const PagedParams& p, hipStream_t stream);
+
+struct SelectParams {
+    PageTableView t;
+    const float* mean;  // [n_pages][Hkv][d]
+    const void* q;      // [B][H][d]
+    int* pages;         // [B][Hkv][S]
+    unsigned long long* keys;  // [B Hkv][max_pages]: scores as ordered whole numbers
+    int S, first, last, H, Hkv, G;
+};
+template <int D, typename T>
+hipError_t launch_paged_select(const SelectParams& p, hipStream_t stream);
+
+}  // namespace eva

@@ -718,3 +718,134 @@ def append_path(cache, k, v, path=None, counts=None, active=None):
     _call(dev, "eva_qappend_path" if isinstance(cache, QuantCache) else "eva_rappend_path", ctypes.byref(s),
           _expect(k, "k", row, dt, dev), _expect(v, "v", row, dt, dev), _expect(path, "path", (B, T), torch.int32, dev),
           _expect(counts, "counts", (B,), torch.int32, dev), T, _expect(active, "active", (B,), torch.int32, dev))
+
+
+# ---- paged cache ---------------------------------------------------------------
+class PageTable:
+    """Which pages of a pool the sequences of a batch have (see eva_page_table in
+    eva.h), shared by all layers' PagedCaches: n_tok [B], table [B, max_pages],
+    the stack free_pages [n_pages] with n_free [1], all int32 on the device.
+    `page`: tokens of a page (16, 32, 64, 128 or 256); `max_tokens` bounds every
+    sequence.  `storage` = (n_tok, table, free_pages, n_free) takes arrays that there
+    are already, as they stand; else every page is free."""
+
+    def __init__(self, B, page, n_pages, max_tokens, device="cuda", storage=None):
+        rows = -(-max_tokens // page)
+        if storage is None:
+            self.n_tok = torch.zeros(B, dtype=torch.int32, device=device)
+            self.table = torch.full((B, rows), -1, dtype=torch.int32, device=device)
+            # the lowest pages on top
+            self.free_pages = torch.arange(n_pages - 1, -1, -1, dtype=torch.int32, device=device)
+            self.n_free = torch.full((1,), n_pages, dtype=torch.int32, device=device)
+        else:
+            self.n_tok, self.table, self.free_pages, self.n_free = storage
+            dev = self.n_tok.get_device()
+            for t, what, shape in ((self.n_tok, "n_tok", (B,)), (self.table, "table", (B, rows)),
+                                   (self.free_pages, "free_pages", (n_pages,)), (self.n_free, "n_free", (1,))):
+                _expect(t, what, shape, torch.int32, dev)
+        self.struct = _lib.EvaPageTableStruct(B=B, P=page, n_pages=n_pages, max_pages=rows,
+                                              **{n: getattr(self, n).data_ptr()
+                                                 for n in ("n_tok", "table", "free_pages", "n_free")})
+        self.ref = ctypes.byref(self.struct)
+
+
+class PagedCache:
+    """A layer's rows in the pages of `table` (see eva_pcache in eva.h): k
+    [n_pages, Hkv, page, d], vt [n_pages, Hkv, page // 8, d, 8] and, unless
+    `means` is false, k_mean [n_pages, Hkv, d] (fp32), which paged_select needs.
+    `storage` = (k, vt, k_mean or None) takes arrays that there are already."""
+
+    def __init__(self, table: PageTable, H, Hkv, d, dtype=torch.bfloat16, means=True, fill=None, storage=None):
+        t, dev = table.struct, table.n_tok.device
+        shapes = ((t.n_pages, Hkv, t.P, d), (t.n_pages, Hkv, t.P // 8, d, 8), (t.n_pages, Hkv, d))
+        if storage is None:
+            mk = (lambda s, dt: torch.full(s, fill, dtype=dt, device=dev)) if fill is not None else \
+                (lambda s, dt: torch.empty(s, dtype=dt, device=dev))
+            self.k, self.vt = mk(shapes[0], dtype), mk(shapes[1], dtype)
+            self.k_mean = mk(shapes[2], torch.float32) if means else None
+        else:
+            self.k, self.vt, self.k_mean = storage
+            for x, what, shape, dt in zip(storage, ("k", "vt", "k_mean"), shapes, (dtype, dtype, torch.float32)):
+                _expect(x, what, shape, dt, table.n_tok.get_device())
+        self.table, self.dtype = table, dtype
+        self.struct = _lib.EvaPCacheStruct(H=H, H_kv=Hkv, d=d, dtype=_DTYPES[dtype], P=t.P, n_pages=t.n_pages,
+                                           k=self.k.data_ptr(), vt=self.vt.data_ptr(), k_mean=_ptr(self.k_mean))
+        self.ref = ctypes.byref(self.struct)
+        self._sizes = {}  # workspace bytes by (call, length of the page list)
+
+    def _ws_bytes(self, name, S):
+        n = self._sizes.get((name, S))
+        if n is None:
+            n = self._sizes[name, S] = getattr(_lib.load(), name)(self.ref, self.table.ref, S)
+        return n
+
+
+def page_extend(table: PageTable, T: int = 1, counts=None):
+    """Pages and slots for counts[b] (int32 [B], at most T; None: T) new tokens of
+    every sequence: (slots [B, T], start [B], granted [B]), int32.  A sequence that the
+    free pages or its row of the table do not suffice for is granted none."""
+    s, dev = table.struct, table.n_tok.get_device()
+    if T < 1:
+        raise ValueError("T must be at least 1")
+    B, n_tok = s.B, table.n_tok
+    c = _expect(counts, "counts", (B,), torch.int32, dev)
+    slots, start = n_tok.new_empty((B, T)), torch.empty_like(n_tok)
+    granted = torch.empty_like(start)
+    _call(dev, "eva_page_extend", table.ref, c, T, slots.data_ptr(), start.data_ptr(), granted.data_ptr())
+    return slots, start, granted
+
+
+def page_truncate(table: PageTable, lens):
+    """Sequence b keeps its first lens[b] (int32 [B]) tokens; pages that none is left
+    in become free.  0: the sequence leaves."""
+    dev = table.n_tok.get_device()
+    _call(dev, "eva_page_truncate", table.ref, _expect(lens, "lens", (table.struct.B,), torch.int32, dev))
+
+
+def paged_append(cache: PagedCache, k, v, slots):
+    """Write new tokens' keys and values [B, Hkv, T, d] (or [B, Hkv, d]) into page_extend's
+    slots [B, T]; pages that they complete get their mean key."""
+    s, dev, dt = cache.struct, cache.k.get_device(), cache.dtype
+    if slots.dim() != 2:
+        raise ValueError("slots must be [B, T]")
+    B, T = slots.shape
+    row = (B, s.H_kv, s.d) if k.dim() == 3 and T == 1 else (B, s.H_kv, T, s.d)
+    _call(dev, "eva_paged_append", cache.ref, _expect(k, "k", row, dt, dev), _expect(v, "v", row, dt, dev),
+          _expect(slots, "slots", (B, T), torch.int32, dev), B, T)
+
+
+def paged_select(cache: PagedCache, q, n_pages: int, first: int = 1, last: int = 1):
+    """The pages that each kv head's queries choose by the pages' mean keys: q
+    [B, H, d] -> int32 [B, Hkv, n_pages], ascending, then -1; the `first` first and the
+    `last` last pages of a sequence are always among them."""
+    s, dev, t = cache.struct, cache.k.get_device(), cache.table
+    B = t.struct.B
+    pq = _expect(q, "q", (B, s.H, s.d), cache.dtype, dev)
+    if n_pages < 1:
+        raise ValueError("n_pages must be at least 1")
+    pages = t.n_tok.new_empty((B, s.H_kv, n_pages))
+    n = cache._ws_bytes("eva_paged_select_workspace_bytes", n_pages)
+    ws = _scratch(q, n)
+    _call(dev, "eva_paged_select", cache.ref, t.ref, pq, n_pages, first, last, pages.data_ptr(), _ptr(ws), n)
+    return pages
+
+
+def paged_decode(cache: PagedCache, q, pages=None, active=None, out=None, use_workspace=True):
+    """Attention of one query a sequence, that of its last token, over all its
+    tokens, or over those of its kv heads' `pages` (int32 [B, Hkv, S], paged_select's):
+    q [B, H, d] -> o [B, H, d].  Rows of sequences without tokens are zeros, those of
+    inactive ones keep the contents of `out`."""
+    s, dev, t = cache.struct, cache.k.get_device(), cache.table
+    B, S = t.struct.B, 0
+    pq = _expect(q, "q", (B, s.H, s.d), cache.dtype, dev)
+    if pages is not None:
+        if pages.dim() != 3 or pages.shape[2] < 1:
+            raise ValueError("pages must be [B, Hkv, S]")
+        S = pages.shape[2]
+    pp = _expect(pages, "pages", (B, s.H_kv, S), torch.int32, dev)
+    on = _expect(active, "active", (B,), torch.int32, dev)
+    o, po = _rows_out(q, out, active is None, dev)
+    n = cache._ws_bytes("eva_paged_decode_workspace_bytes", S) if use_workspace else 0
+    ws = _scratch(q, n)
+    _call(dev, "eva_paged_decode", cache.ref, t.ref, pq, po, pp, S, on, _ptr(ws), n)
+    return o
