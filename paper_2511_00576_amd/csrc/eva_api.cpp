@@ -1306,7 +1306,8 @@ int paged_route(PagedRoute& r, const eva_pcache* c, const eva_page_table* t, int
     r.n_hg = (c->H / c->H_kv + 15) / 16;
     r.rows = (long long)t->B * c->H_kv * r.n_hg;
     const long long pages = S > 0 && S < t->max_pages ? S : t->max_pages;
-    const long long chunks = pages * t->P <= 32 ? 1 : pages * t->P / 32 + (pages * t->P % 32 != 0);
+    const int tokens = 16 * eva::paged_blocks(c->d, c->dtype == EVA_F32 ? 4 : 2);
+    const long long chunks = (pages * t->P + tokens - 1) / tokens;
     if (r.rows * chunks > 0x7fffffffLL || r.rows > 0x7fffff) return EVA_ERR_UNSUPPORTED;
     r.wgs = 0;
     if (chunks > eva::kPagedMinPart) {

@@ -2,7 +2,7 @@
 // those of a list of pages.
 //
 // A row is (sequence, kv head, group of up to 16 query heads); its keys go by
-// chunks of 32 tokens, each two halves of 16 that lie in one page each.  Per
+// chunks of one or two blocks of 16 tokens, each of which lies in one page.  Per
 // chunk a wave computes S^T = K Q^T and O^T += V^T P^T on the matrix cores with
 // the operands read straight from memory, 16 bytes a lane, the softmax's maximum
 // and sum running: every key and value is read once for the heads that share it.
@@ -19,7 +19,10 @@ namespace eva {
 namespace {
 
 constexpr float kPagedTau = 8.f;  // log2 units: unscaled weights stay <= 256
-constexpr int kPagedWaves = 4;
+#ifndef NWV
+#define NWV 4
+#endif
+constexpr int kPagedWaves = NWV;
 
 // Pages that a row's query attends, of a sequence of n tokens: all it has, or the
 // first so many of its list.
@@ -29,17 +32,11 @@ __device__ __forceinline__ int row_pages(const PagedParams& a, int n) {
 }
 // Chunks of a row; at least one, which writes the zeros of a sequence without tokens;
 // none for an inactive one.
-__device__ __forceinline__ int row_chunks(const PagedParams& a, int b) {
+template <int TOKENS>
+__device__ __forceinline__ int row_chunks(const PagedParams& a, int b, int n) {
     if (a.active && a.active[b] == 0) return 0;
-    const int n = held_tokens(a.t, b);
     const int len = a.pages ? row_pages(a, n) << a.t.shift : n;
-    return max((len + 31) >> 5, 1);
-}
-
-__device__ __forceinline__ int wave_sum(int x) {
-#pragma unroll
-    for (int i = 32; i; i >>= 1) x += __shfl_xor(x, i);
-    return x;
+    return max((len + TOKENS - 1) / TOKENS, 1);
 }
 
 // A word that every lane wants and that nothing writes during the launch: through the
@@ -49,30 +46,41 @@ __device__ __forceinline__ int scalar_load(const int* p) {
 }
 
 // 16 tokens of a page.
-struct Half {
+struct Block {
     size_t at;  // elements from the pool's start to their rows (keys and values alike)
-    int valid;  // of them, the first so many are attended
+    int left;   // tokens of the sequence from the first of them on
+    int valid;  // of the block's, the first so many are attended
     bool lost;  // the table names no page of the pool
 };
 
-// Half h of chunk ch of the row (b, kvh).
-template <int D>
-__device__ __forceinline__ Half locate(const PagedParams& a, int b, int kvh, int n, int n_pages, int ch, int h) {
+// Chunk `chunk` of NB blocks of the row (b, kvh).  Pages hold whole chunks, but for
+// those of 16 tokens where NB is 2.
+template <int D, int NB>
+__device__ __forceinline__ void locate(Block (&x)[NB], const PagedParams& a, int b, int kvh, int n, int n_pages, int chunk) {
     const int shift = a.t.shift;
-    const int v = ch * 32 + h * 16, e = v >> shift, off = v & ((1 << shift) - 1);
-    Half r{0, 0, false};
-    if (e < n_pages) {
-        int lp = e;
-        if (a.pages) lp = scalar_load(a.pages + ((size_t)b * a.Hkv + kvh) * a.S + e);
-        const int left = n - ((lp << shift) + off);
-        if ((unsigned)lp < (unsigned)pages_of(n, shift) && left > 0) {
-            const int page = scalar_load(a.t.table + (size_t)b * a.t.max_pages + lp);
-            r.valid = min(left, 16);
-            r.lost = (unsigned)page >= (unsigned)a.t.n_pages;
-            r.at = (((size_t)(r.lost ? 0 : page) * a.Hkv + kvh) << shift) * D + (size_t)off * D;
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+        if (i > 0 && shift > 4) {
+            x[i].at = x[0].at + 16 * i * D;
+            x[i].valid = max(min(x[0].left - 16 * i, 16), 0);
+            x[i].lost = x[0].lost;
+            continue;
+        }
+        const int v = (chunk * NB + i) * 16, e = v >> shift, off = v & ((1 << shift) - 1);
+        x[i] = Block{};
+        if (e < n_pages) {
+            int lp = e;
+            if (a.pages) lp = scalar_load(a.pages + ((size_t)b * a.Hkv + kvh) * a.S + e);
+            const int left = n - ((lp << shift) + off);
+            if ((unsigned)lp < (unsigned)pages_of(n, shift) && left > 0) {
+                const int page = scalar_load(a.t.table + (size_t)b * a.t.max_pages + lp);
+                x[i].left = left;
+                x[i].valid = min(left, 16);
+                x[i].lost = (unsigned)page >= (unsigned)a.t.n_pages;
+                x[i].at = ((((size_t)(x[i].lost ? 0 : page) * a.Hkv + kvh) << shift) + off) * D;
+            }
         }
     }
-    return r;
 }
 
 // The running state of a wave: 16 columns, per lane (g, c16) the features
@@ -89,9 +97,13 @@ struct RowState {
     }
     // Scores of a chunk (two blocks of four per lane) become weights; the reference
     // maximum moves only when the chunk's exceeds it by more than kPagedTau.
-    __device__ __forceinline__ void weigh(floatx4 (&s)[2], float scale) {
-        float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
-                         fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+    template <int NB>
+    __device__ __forceinline__ void weigh(floatx4 (&s)[NB], float scale) {
+        float mx = s[0][0];
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[kb][i]);
         mx = xgroup_max(mx) * scale;
         const bool raise = mx > m + kPagedTau;
         if (__builtin_amdgcn_ballot_w64(raise)) {
@@ -105,7 +117,7 @@ struct RowState {
         // no maximum yet (scores of -inf alone): their weights are 0
         const float off = m == -INFINITY ? 0.f : -m;
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
+        for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 s[kb][i] = fast_exp2(fmaf(s[kb][i], scale, off));
@@ -121,6 +133,7 @@ struct Chunk;
 
 template <int D>
 struct Chunk<D, bf16> {
+    static constexpr int kBlocks = 2;
     bf16x8 k[2][D / 32], v[D / 16];
     // Rows are permuted so that the eight scores of a lane are keys 8g .. 8g + 7 (block kb:
     // + 4 kb + i), the slots of its 16 bytes of a feature's values.
@@ -129,14 +142,16 @@ struct Chunk<D, bf16> {
         for (int i = 0; i < D / 32; ++i) q[i] = *reinterpret_cast<const bf16x8*>(row + 32 * i + 8 * g);
     }
     static __device__ __forceinline__ int mask_of(uint32_t bits, int g, int kb) { return (int)(bits >> (8 * g + 4 * kb)) & 15; }
-    __device__ __forceinline__ void load(const bf16* kp, const bf16* vp, size_t at0, size_t at1, int g, int c) {
-        const bf16* kr = kp + (c >= 8 ? at1 : at0) + ((c >> 2 & 1) * 8 + (c & 3)) * D + 8 * g;
-        const bf16* vr = vp + (g >= 2 ? at1 : at0) + vt_index<D>(c, 8 * (g & 1));
+    __device__ __forceinline__ void load_keys(const bf16* kp, const Block (&x)[2], int g, int c) {
+        const bf16* kr = kp + (c >= 8 ? x[1].at : x[0].at) + ((c >> 2 & 1) * 8 + (c & 3)) * D + 8 * g;
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
             for (int i = 0; i < D / 32; ++i)
                 k[kb][i] = __builtin_nontemporal_load(reinterpret_cast<const bf16x8*>(kr + 4 * kb * D + 32 * i));
+    }
+    __device__ __forceinline__ void load_values(const bf16* vp, const Block (&x)[2], int g, int c) {
+        const bf16* vr = vp + (g >= 2 ? x[1].at : x[0].at) + vt_index<D>(c, 8 * (g & 1));
 #pragma unroll
         for (int i = 0; i < D / 16; ++i)
             v[i] = __builtin_nontemporal_load(reinterpret_cast<const bf16x8*>(vr + 16 * i * kVtTile));
@@ -178,7 +193,9 @@ struct Chunk<D, bf16> {
 
 template <int D>
 struct Chunk<D, float> {
-    floatx4 k[2][D / 16], v[2][D / 16];
+    static constexpr int NB = paged_blocks(D, sizeof(float));
+    static constexpr int kBlocks = NB;
+    floatx4 k[NB][D / 16], v[NB][D / 16];
     // Contraction step (i, e) of the scores: feature 16 i + 4 g + e; of the values: key
     // 16 kb + 4 g + e, whose weight the lane holds already.
     static __device__ __forceinline__ void query(floatx4 (&q)[D / 16], const float* row, int g) {
@@ -186,25 +203,27 @@ struct Chunk<D, float> {
         for (int i = 0; i < D / 16; ++i) q[i] = *reinterpret_cast<const floatx4*>(row + 16 * i + 4 * g);
     }
     static __device__ __forceinline__ int mask_of(uint32_t bits, int g, int kb) { return (int)(bits >> (16 * kb + 4 * g)) & 15; }
-    __device__ __forceinline__ void load(const float* kp, const float* vp, size_t at0, size_t at1, int g, int c) {
+    __device__ __forceinline__ void load_keys(const float* kp, const Block (&x)[NB], int g, int c) {
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-            const float* kr = kp + (kb ? at1 : at0) + c * D + 4 * g;
+        for (int kb = 0; kb < NB; ++kb) {
+            const float* kr = kp + x[kb].at + c * D + 4 * g;
 #pragma unroll
             for (int i = 0; i < D / 16; ++i)
                 k[kb][i] = __builtin_nontemporal_load(reinterpret_cast<const floatx4*>(kr + 16 * i));
         }
+    }
+    __device__ __forceinline__ void load_values(const float* vp, const Block (&x)[NB], int g, int c) {
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-            const float* vr = vp + (kb ? at1 : at0) + vt_index<D>(c, 4 * g);
+        for (int kb = 0; kb < NB; ++kb) {
+            const float* vr = vp + x[kb].at + vt_index<D>(c, 4 * g);
 #pragma unroll
             for (int i = 0; i < D / 16; ++i)
                 v[kb][i] = __builtin_nontemporal_load(reinterpret_cast<const floatx4*>(vr + 16 * i * kVtTile));
         }
     }
-    __device__ __forceinline__ void scores(const floatx4 (&q)[D / 16], floatx4 (&s)[2]) const {
+    __device__ __forceinline__ void scores(const floatx4 (&q)[D / 16], floatx4 (&s)[NB]) const {
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
+        for (int kb = 0; kb < NB; ++kb) {
             s[kb] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < D / 16; ++i)
@@ -214,7 +233,7 @@ struct Chunk<D, float> {
     }
     __device__ __forceinline__ void keep_values(uint32_t valid, int g) {
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
+        for (int kb = 0; kb < NB; ++kb) {
             const int m = mask_of(valid, g, kb);
 #pragma unroll
             for (int i = 0; i < D / 16; ++i)
@@ -222,11 +241,11 @@ struct Chunk<D, float> {
                 for (int e = 0; e < 4; ++e) v[kb][i][e] = m >> e & 1 ? v[kb][i][e] : 0.f;
         }
     }
-    __device__ __forceinline__ void add(const floatx4 (&p)[2], floatx4 (&acc)[D / 16]) const {
+    __device__ __forceinline__ void add(const floatx4 (&p)[NB], floatx4 (&acc)[D / 16]) const {
 #pragma unroll
         for (int i = 0; i < D / 16; ++i)
 #pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
+            for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) acc[i] = mfma_f32(v[kb][i][e], p[kb][e], acc[i]);
     }
@@ -270,11 +289,12 @@ __host__ __device__ constexpr int share_floats() { return 16 * (D + 2); }
 __device__ __forceinline__ float* shares_of(const PagedParams& a) { return a.ws + (a.rows + 1) / 2 * 4; }
 
 template <int D, typename T>
-__global__ __launch_bounds__(kPagedWaves * 64) void paged_decode_kernel(PagedParams a) {
+__global__ __launch_bounds__(kPagedWaves * 64) __attribute__((amdgpu_waves_per_eu(3, 8))) void paged_decode_kernel(PagedParams a) {
     constexpr int NW = kPagedWaves;
     constexpr int COL = D + 4;  // 16 columns on distinct banks
     typedef typename QueryFragment<T>::type Frag;
     constexpr int NQ = D / QueryFragment<T>::kFeatures;
+    constexpr int NB = Chunk<D, T>::kBlocks;
     __shared__ float red_m[NW][16], red_l[NW][16];
     __shared__ __attribute__((aligned(16))) float red_o[NW][16][COL];
 
@@ -285,44 +305,48 @@ __global__ __launch_bounds__(kPagedWaves * 64) void paged_decode_kernel(PagedPar
     const T* kp = static_cast<const T*>(a.k);
     const T* vp = static_cast<const T*>(a.vt);
 
-    // this workgroup's chunks: `todo` from chunk c0 of row `row` of sequence b on
-    int b, row, c0, todo, part = 0;
+    // this workgroup's chunks: `todo` from chunk c0 of row `row` of sequence b on.  The
+    // lanes hold 64 sequences' counts at a time, w0 the first of them.
+    int b, row, c0, todo, part = 0, w0, tokens, chunk_of;
+    auto window = [&](int from) {
+        w0 = from;
+        const int i = min(from + lane, a.t.B - 1);
+        tokens = held_tokens(a.t, i);
+        chunk_of = from + lane < a.t.B ? row_chunks<16 * NB>(a, i, tokens) : 0;
+    };
     if (a.ws) {
-        int total = 0;
-        for (int i = 0; i < a.t.B; i += 64) total += i + lane < a.t.B ? row_chunks(a, i + lane) : 0;
-        total = wave_sum(total) * unit;
+        window(0);
+        int total = chunk_of;
+        for (int i = 64; i < a.t.B; i += 64)
+            if (i + lane < a.t.B) total += row_chunks<16 * NB>(a, i + lane, held_tokens(a.t, i + lane));
+        total = __builtin_amdgcn_readlane(wave_scan(total), 63) * unit;
         part = max((total + a.wgs - 1) / a.wgs, kPagedMinPart);
         const int from = (int)blockIdx.x * part;
         if (from >= total) return;
         todo = min(part, total - from);
         // the sequence that holds chunk `from`
-        int before = 0, at = 0;
-        for (int i = 0;; i += 64) {
-            const int mine = i + lane < a.t.B ? row_chunks(a, i + lane) * unit : 0;
-            int upto = mine;
-#pragma unroll
-            for (int s = 1; s < 64; s <<= 1) {
-                const int y = __shfl_up(upto, s);
-                if (lane >= s) upto += y;
-            }
-            upto += before;
+        int before = 0, at;
+        while (true) {
+            const int upto = before + wave_scan(chunk_of * unit);
             const unsigned long long past = __builtin_amdgcn_ballot_w64(upto > from);
             if (past) {
                 const int l = __builtin_ctzll(past);
-                b = i + l;
-                at = from - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(mine, l));
+                b = w0 + l;
+                at = from - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(chunk_of, l) * unit);
                 break;
             }
             before = __builtin_amdgcn_readlane(upto, 63);
+            window(w0 + 64);
         }
-        const int chunks = row_chunks(a, b);
+        const int chunks = __builtin_amdgcn_readlane(chunk_of, b - w0);
         row = at / chunks;
         c0 = at - row * chunks;
     } else {
         b = (int)blockIdx.x / a.f_unit;
         row = (int)blockIdx.x % a.f_unit;
         c0 = 0;
-        todo = row_chunks(a, b);
+        window(b / 64 * 64);
+        todo = __builtin_amdgcn_readlane(chunk_of, b - w0);
         if (todo == 0) return;
     }
     b = __builtin_amdgcn_readfirstlane(b);
@@ -331,9 +355,9 @@ __global__ __launch_bounds__(kPagedWaves * 64) void paged_decode_kernel(PagedPar
     todo = __builtin_amdgcn_readfirstlane(todo);
 
     for (bool first = true;; first = false) {
-        const int n = __builtin_amdgcn_readfirstlane(held_tokens(a.t, b));
+        const int n = __builtin_amdgcn_readlane(tokens, b - w0);
         const int n_pages = row_pages(a, n);
-        const int chunks = __builtin_amdgcn_readfirstlane(row_chunks(a, b));
+        const int chunks = __builtin_amdgcn_readlane(chunk_of, b - w0);
         const int c1 = min(chunks, c0 + todo);
         const int kvh = row / a.f_hg, hg = row % a.f_hg;
         const int h0 = kvh * a.G + hg * 16;
@@ -345,39 +369,45 @@ __global__ __launch_bounds__(kPagedWaves * 64) void paged_decode_kernel(PagedPar
         RowState<D> st;
         st.clear();
         bool any = false;
+        // a chunk's keys are requested while the one before is weighed, its values once
+        // that one's have been used: the wave always has half a chunk in flight
+        Chunk<D, T> rows;
+        Block x[NB];
         int ch = c0 + wave;
-        Half x0{0, 0, false}, x1{0, 0, false};
         if (ch < c1) {
-            x0 = locate<D>(a, b, kvh, n, n_pages, ch, 0);
-            x1 = locate<D>(a, b, kvh, n, n_pages, ch, 1);
+            locate<D, NB>(x, a, b, kvh, n, n_pages, ch);
+            rows.load_keys(kp, x, g, c16);
+            rows.load_values(vp, x, g, c16);
         }
         while (ch < c1) {
-            Chunk<D, T> x;
-            x.load(kp, vp, x0.at, x1.at, g, c16);
-            const uint32_t valid = (x0.valid ? 0xffffu >> (16 - x0.valid) : 0u) |
-                                   (x1.valid ? 0xffff0000u >> (16 - x1.valid) & 0xffff0000u : 0u);
-            const bool lost0 = x0.lost, lost1 = x1.lost;
-            ch += NW;
-            if (ch < c1) {
-                x0 = locate<D>(a, b, kvh, n, n_pages, ch, 0);
-                x1 = locate<D>(a, b, kvh, n, n_pages, ch, 1);
-            }
-            if (valid == 0) continue;
-            any = true;
-            floatx4 s[2];
-            x.scores(q, s);
-            if (valid != 0xffffffffu || lost0 || lost1) {
-                const uint32_t lost = (lost0 ? 0xffffu : 0u) | (lost1 ? 0xffff0000u : 0u);
+            // a bit for each token that is attended, and for each whose page there is not
+            uint32_t valid = 0, lost = 0;
 #pragma unroll
-                for (int kb = 0; kb < 2; ++kb) {
+            for (int i = 0; i < NB; ++i) {
+                valid |= ((1u << x[i].valid) - 1) << (16 * i);
+                lost |= (x[i].lost ? 0xffffu : 0u) << (16 * i);
+            }
+            any = any || valid != 0;
+            ch += NW;
+            const bool more = ch < c1;
+            if (more) locate<D, NB>(x, a, b, kvh, n, n_pages, ch);
+            floatx4 s[NB];
+            rows.scores(q, s);
+            __builtin_amdgcn_sched_barrier(0);
+            if (more) rows.load_keys(kp, x, g, c16);
+            if (valid != 0xffffffffu >> (32 - 16 * NB) || lost) {
+#pragma unroll
+                for (int kb = 0; kb < NB; ++kb) {
                     const int in = Chunk<D, T>::mask_of(valid, g, kb), no = Chunk<D, T>::mask_of(lost, g, kb);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) s[kb][i] = in >> i & 1 ? no >> i & 1 ? NAN : s[kb][i] : -INFINITY;
                 }
-                x.keep_values(valid, g);
+                rows.keep_values(valid, g);
             }
             st.weigh(s, a.scale_log2);
-            x.add(s, st.acc);
+            rows.add(s, st.acc);
+            __builtin_amdgcn_sched_barrier(0);
+            if (more) rows.load_values(vp, x, g, c16);
         }
 
         // ---- the waves' parts of the row ----
@@ -431,9 +461,9 @@ __global__ __launch_bounds__(kPagedWaves * 64) void paged_decode_kernel(PagedPar
         c0 = 0;
         if (++row == unit) {
             row = 0;
-            do ++b;  // todo > 0: there is one
-            while (row_chunks(a, b) == 0);
-            b = __builtin_amdgcn_readfirstlane(b);
+            do {  // todo > 0: there is one
+                if (++b == w0 + 64) window(b);
+            } while (__builtin_amdgcn_readlane(chunk_of, b - w0) == 0);
         }
         __syncthreads();  // the parts have been read
     }
@@ -448,7 +478,7 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedParams a)
     __shared__ __attribute__((aligned(16))) floatx4 red_o[kJoinThreads];
     const int row = blockIdx.x;
     const int b = row / a.f_unit;
-    if (row_chunks(a, b) == 0) return;  // inactive
+    if (a.active && a.active[b] == 0) return;  // no one has written its entry
     const int2 info = reinterpret_cast<const int2*>(a.ws)[row];
     if (info.x < 0) return;
     const int kvh = row % a.f_unit / a.f_hg, hg = row % a.f_unit % a.f_hg;
@@ -457,13 +487,12 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedParams a)
     const float* first = shares_of(a) + (size_t)info.x * share_floats<D>();
     const float* rest = shares_of(a) + (size_t)((info.x >> 1) + 1) * 2 * share_floats<D>();
     const int items = ncols * (D / 4);  // 16 .. 512
-    const int groups = kJoinThreads / items;
+    constexpr int NB = 8;  // shares whose loads are in flight together
+    const int groups = min(kJoinThreads / items, (shares + NB - 1) / NB);
     const int grp = threadIdx.x / items, e = threadIdx.x % items;
     const int col = e / (D / 4), f = e % (D / 4) * 4;
     float M = -INFINITY, L = 0.f;
     floatx4 O = {0.f, 0.f, 0.f, 0.f};
-    // NB shares' loads in flight together
-    constexpr int NB = 4;
     if (grp < groups) {
         for (int s0 = grp; s0 < shares; s0 += groups * NB) {
             float m[NB], l[NB];

@@ -28,6 +28,48 @@ __host__ __device__ __forceinline__ int pages_of(int tokens, int shift) {
     return (int)(((unsigned)tokens + (1u << shift) - 1) >> shift);
 }
 
+// Data movement between lanes in one VALU instruction (a shuffle goes through LDS, 100
+// cycles and more); lanes that have no source get 0.
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ int dpp(int x) {
+    return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false);
+}
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ long long dpp(long long x) {
+    const unsigned lo = (unsigned)dpp<CTRL, ROWS>((int)x);
+    return (long long)((unsigned long long)(unsigned)dpp<CTRL, ROWS>((int)(x >> 32)) << 32 | lo);
+}
+// Inclusive sum over the wave: within rows of 16 lanes, then from row to row.
+template <typename I>
+__device__ __forceinline__ I wave_scan(I x) {
+    x += dpp<0x111>(x);       // one lane up
+    x += dpp<0x112>(x);       // two
+    x += dpp<0x114>(x);       // four
+    x += dpp<0x118>(x);       // eight
+    x += dpp<0x142, 0xa>(x);  // rows 0 and 2 to the next
+    x += dpp<0x143, 0xc>(x);  // the first two rows to the others
+    return x;
+}
+
+// Inclusive sum over the workgroup's threads, and the whole sum; sums has room for
+// every wave's.
+template <typename I>
+__device__ __forceinline__ I block_scan(I x, I* sums, I& total) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    x = wave_scan(x);
+    __syncthreads();  // the last use of sums is over
+    if (lane == 63) sums[wave] = x;
+    __syncthreads();
+    I before = 0;
+    total = 0;
+    for (int w = 0; w < waves; ++w) {
+        const I s = sums[w];
+        if (w < wave) before += s;
+        total += s;
+    }
+    return x + before;
+}
+
 hipError_t launch_page_truncate(const PageTableView& t, const int* lens, hipStream_t stream);
 // slots [B][T], start [B], granted [B]
 hipError_t launch_page_extend(const PageTableView& t, const int* counts, int T, int* slots, int* start, int* granted,
@@ -61,10 +103,13 @@ struct PagedParams {
     FastDiv f_unit, f_hg;  // divisors of Hkv n_hg and of n_hg
     float scale_log2;
 };
+// Blocks of 16 tokens in a chunk, what a wave requests at once: 16 KB of keys and
+// values, 64 registers a lane (two blocks of fp32 rows of 128 features would take 128).
+constexpr int paged_blocks(int d, int bytes) { return bytes == 4 && d == 128 ? 1 : 2; }
 // The fewest chunks a workgroup takes: one for each of its four waves.
 constexpr int kPagedMinPart = 4;
 // Workgroups that share a decode's chunks: as many as the CUs hold at once.
-constexpr int kPagedWgs = 768;
+constexpr int kPagedWgs = 512;
 // Bytes of the workspace: a pair of ints per row, then two shares per workgroup.
 inline size_t paged_ws_bytes(long long rows, long long wgs, int d) {
     return ((size_t)(rows + 1) / 2 * 4 + (size_t)wgs * 2 * 16 * (d + 2)) * sizeof(float);

@@ -13,13 +13,13 @@ namespace eva {
 
 namespace {
 
-typedef double doublex4 __attribute__((ext_vector_type(4)));
-
 constexpr int kScoreWaves = 4;
 constexpr int kChooseThreads = 512;
 // Scores held in LDS by the choosing workgroup; longer rows are read again from memory.
 constexpr int kChooseLds = 4096;
 constexpr int kBins = 2048;  // 11 bits a pass
+// Scores of the bin in which the choice ends that are ranked one against the other.
+constexpr int kMaxTied = 256;
 
 // Order of the scores as whole numbers: -0 and 0 alike, NaN above all (so that what it
 // stands for reaches the output).
@@ -28,6 +28,22 @@ __device__ __forceinline__ unsigned long long ordered(double x) {
     x = x + 0.0;
     const unsigned long long u = __builtin_bit_cast(unsigned long long, x);
     return u >> 63 ? ~u : u | 1ull << 63;
+}
+
+// The score again; bits that no score has (NaN) stay one.
+__device__ __forceinline__ double score_of(unsigned long long k) {
+    return __builtin_bit_cast(double, k >> 63 ? k & ~(1ull << 63) : ~k);
+}
+
+__device__ __forceinline__ void load4(const float* p, float (&x)[4]) {
+    const floatx4 v = *reinterpret_cast<const floatx4*>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = v[i];
+}
+__device__ __forceinline__ void load4(const bf16* p, float (&x)[4]) {
+    const bf16x4 v = *reinterpret_cast<const bf16x4*>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = (float)v[i];
 }
 
 // Pages of sequence b that are ranked: [lo, hi).  None where all are kept.
@@ -39,92 +55,124 @@ __device__ __forceinline__ void ranked(const SelectParams& a, int held, int& lo,
     }
 }
 
-// One wave scores 16 pages: A = their mean keys, B = 16 query heads, contraction step (i, e)
-// of lane group g feature 16 i + 4 g + e, so that both are 16-byte loads.  D: lane (g, c)
-// holds pages 4 r + g (r = 0 .. 3) for head c.  Bound by the mean keys' read.
+// One wave scores 16 pages for four query heads at a time, with the matrix core's four
+// products of 4 x 4 x 4: block c / 4 holds pages 4 (c / 4) + 0 .. 3 and all four the same heads,
+//     A lane (g, c): page c, B: head c % 4, both contraction index g, which is feature
+//     16 i + 4 g + e in step (i, e), so that the mean keys are 16-byte loads;
+//     D lane (g, c): page 4 (c / 4) + g, head c % 4.
+// (The 16 x 16 x 4 product, at the same rate, would spend three quarters of its columns on
+// heads that there are not: 22 us against 11 us for 256 rows of 513 pages, d = 128.)
+// Bound by the mean keys' read and the chain count -> table -> mean.
 template <int D, typename T>
 __global__ __launch_bounds__(kScoreWaves * 64) void paged_score_kernel(SelectParams a) {
     const int b = (int)blockIdx.y / a.Hkv, kvh = (int)blockIdx.y % a.Hkv;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int g = lane >> 4, c = lane & 15;
+    const T* heads = static_cast<const T*>(a.q) + ((size_t)b * a.H + (size_t)kvh * a.G) * D + 4 * g;
+    // the heads h0 .. h0 + 3; past the last they repeat it, which changes no maximum
+    double q[D / 4];
+    auto load_heads = [&](int h0) {
+        const T* row = heads + (size_t)min(h0 + (c & 3), a.G - 1) * D;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) {
+            float x[4];
+            load4(row + 16 * i, x);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) q[4 * i + e] = (double)x[e];
+        }
+    };
+    const int step = gridDim.x * kScoreWaves * 16;
+    int j0 = ((int)blockIdx.x * kScoreWaves + wave) * 16;  // from the first ranked page on
+    // a tile's pages are looked up one tile ahead, the first before the sequence's length is
+    // known (any entry of its row may be read; what it names is checked below)
+    const int* row = a.t.table + (size_t)b * a.t.max_pages;
+    auto look_up = [&](int j) { return row[min(a.first + j + c, a.t.max_pages - 1)]; };
+    int next = look_up(j0);
+    load_heads(0);
     const int held = pages_of(held_tokens(a.t, b), a.t.shift);
     int lo, hi;
     ranked(a, held, lo, hi);
-    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int g = lane >> 4, c = lane & 15;
-    const int step = gridDim.x * kScoreWaves * 16;
-    for (int j0 = lo + ((int)blockIdx.x * kScoreWaves + wave) * 16; j0 < hi; j0 += step) {
-        // rows past the last repeat it
-        const int page = a.t.table[(size_t)b * a.t.max_pages + min(j0 + c, hi - 1)];
+    for (; j0 < hi - lo; j0 += step) {
+        const int page = next;
         const bool lost = (unsigned)page >= (unsigned)a.t.n_pages;
         const float* mean = a.mean + ((size_t)(lost ? 0 : page) * a.Hkv + kvh) * D + 4 * g;
         floatx4 m[D / 16];
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) m[i] = *reinterpret_cast<const floatx4*>(mean + 16 * i);
+        if (j0 + step < hi - lo) next = look_up(j0 + step);
         const unsigned long long lost_rows = __builtin_amdgcn_ballot_w64(lost);
-        unsigned long long best[4] = {0, 0, 0, 0};
-        for (int h0 = 0; h0 < a.G; h0 += 16) {
-            const T* q = static_cast<const T*>(a.q) + ((size_t)b * a.H + kvh * a.G + min(h0 + c, a.G - 1)) * D + 4 * g;
-            doublex4 acc = {0., 0., 0., 0.};
+        unsigned long long best = 0;
+        for (int h0 = 0; h0 < a.G; h0 += 4) {
+            if (a.G > 4) load_heads(h0);
+            double acc = 0.;
 #pragma unroll
             for (int i = 0; i < D / 16; ++i)
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    acc = __builtin_amdgcn_mfma_f64_16x16x4f64((double)m[i][e], (double)to_f32(q[16 * i + e]), acc, 0, 0, 0);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const unsigned long long k = ordered(acc[r]);
-                best[r] = k > best[r] ? k : best[r];
-            }
+                    acc = __builtin_amdgcn_mfma_f64_4x4x4f64((double)m[i][e], q[4 * i + e], acc, 0, 0, 0);
+            const unsigned long long k = ordered(acc);
+            best = k > best ? k : best;
         }
-        unsigned long long* out = a.keys + (size_t)blockIdx.y * a.t.max_pages;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-#pragma unroll
-            for (int s = 1; s < 16; s <<= 1) {
-                const unsigned long long k = __shfl_xor(best[r], s);
-                best[r] = k > best[r] ? k : best[r];
-            }
-            const int j = 4 * r + g;
-            // a page that the pool does not have ranks first: its row becomes NaN
-            if (c == 0 && j0 + j < hi) out[j0 + j] = lost_rows >> j & 1 ? ~0ull : best[r];
-        }
+        unsigned long long other = (unsigned long long)dpp<0xb1>((long long)best);  // lanes 1 0 3 2 of a quad
+        best = other > best ? other : best;
+        other = (unsigned long long)dpp<0x4e>((long long)best);                     // 2 3 0 1
+        best = other > best ? other : best;
+        const int j = (c & 12) + g;
+        // a page that the pool does not have ranks first: its row becomes NaN
+        if ((c & 3) == 0 && j0 + j < hi - lo)
+            a.keys[(size_t)blockIdx.y * a.t.max_pages + j0 + j] = lost_rows >> j & 1 ? ~0ull : best;
     }
 }
 
-// Inclusive sum over the workgroup's threads, and the whole sum.
-__device__ __forceinline__ int scan(int x, int* sums, int& total) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// Of a workgroup's bins, the one in which the `want`-th highest score lies: each thread
+// sums neighbouring bins from the top.
+struct Found {
+    int bin, above, count;  // scores in higher bins, and in this one
+};
+__device__ __forceinline__ void find_bin(const int* bins, int want, int* sums, Found* found) {
+    constexpr int EACH = kBins / kChooseThreads;
+    const int top = kBins - 1 - (int)threadIdx.x * EACH;
+    int mine = 0;
 #pragma unroll
-    for (int i = 1; i < 64; i <<= 1) {
-        const int y = __shfl_up(x, i);
-        if (lane >= i) x += y;
+    for (int i = 0; i < EACH; ++i) mine += bins[top - i];
+    int total;
+    const int upto = block_scan(mine, sums, total);
+    if (upto >= want && upto - mine < want) {
+        int above = upto - mine;
+        for (int i = 0; i < EACH; ++i) {
+            if (above + bins[top - i] >= want) {
+                *found = Found{top - i, above, bins[top - i]};
+                break;
+            }
+            above += bins[top - i];
+        }
     }
-    __syncthreads();  // the last use of sums is over
-    if (lane == 63) sums[wave] = x;
     __syncthreads();
-    int before = 0;
-    total = 0;
-    for (int w = 0; w < kChooseThreads / 64; ++w) {
-        const int s = sums[w];
-        if (w < wave) before += s;
-        total += s;
-    }
-    return x + before;
 }
 
-// A workgroup per (sequence, kv head): the k-th largest score by a radix search, 11 bits
-// a pass, which ends as soon as a bin holds as many scores as are still wanted (two or
-// three passes for scores that differ); then the pages in their order.
+// A workgroup per (sequence, kv head).  The scores are counted in bins of equal width
+// between the lowest and the highest (a map that keeps their order), which spreads them; the
+// `want`-th highest lies in one bin, whose few scores are ranked one against the other.
+// Where it holds many (scores that tie, or one far from all others), a radix search
+// over the bits finds it instead, 11 a pass.  Then the pages in their order.  Bound by
+// the passes' barriers.
 __global__ __launch_bounds__(kChooseThreads) void paged_choose_kernel(SelectParams a) {
     __shared__ unsigned long long sh_keys[kChooseLds];
     __shared__ int bins[kBins];
-    __shared__ int sums[kChooseThreads / 64];
-    __shared__ int sh_bin, sh_above, sh_count;
+    __shared__ long long sums[kChooseThreads / 64];
+    __shared__ double sh_lo[kChooseThreads / 64], sh_hi[kChooseThreads / 64];
+    __shared__ unsigned long long tied[kMaxTied];
+    __shared__ int tied_at[kMaxTied];
+    __shared__ Found found;
+    __shared__ int sh_n, sh_want;
+    __shared__ unsigned long long sh_key;
+    int* isums = reinterpret_cast<int*>(sums);
     const int b = (int)blockIdx.x / a.Hkv, tid = threadIdx.x;
     const int held = pages_of(held_tokens(a.t, b), a.t.shift);
     int lo, hi;
     ranked(a, held, lo, hi);
     int* out = a.pages + (size_t)blockIdx.x * a.S;
-    if (hi == lo && held <= a.S) {  // all of them
+    if (held <= a.S) {  // all of them
         for (int i = tid; i < a.S; i += kChooseThreads) out[i] = i < held ? i : -1;
         return;
     }
@@ -133,16 +181,84 @@ __global__ __launch_bounds__(kChooseThreads) void paged_choose_kernel(SelectPara
     const int n = hi - lo;
     int want = a.S - a.first - a.last;
     if (want == 0) return;
-    const unsigned long long* gkeys = a.keys + (size_t)blockIdx.x * a.t.max_pages + lo;
+    const unsigned long long* gkeys = a.keys + (size_t)blockIdx.x * a.t.max_pages;
     const bool in_lds = n <= kChooseLds;
-    if (in_lds)
-        for (int i = tid; i < n; i += kChooseThreads) sh_keys[i] = gkeys[i];
     auto key = [&](int i) { return in_lds ? sh_keys[i] : gkeys[i]; };
-    // scores whose bits from `shift` on are `prefix` are still open; all above it are taken
+
+    // the finite scores' range
+    double low = INFINITY, high = -INFINITY;
+    for (int i = tid; i < n; i += kChooseThreads) {
+        const unsigned long long k = gkeys[i];
+        if (in_lds) sh_keys[i] = k;
+        const double x = score_of(k);
+        if (__builtin_fabs(x) < INFINITY) {
+            low = fmin(low, x);
+            high = fmax(high, x);
+        }
+    }
+    for (int i = tid; i < kBins; i += kChooseThreads) bins[i] = 0;
+    if (tid == 0) sh_n = 0;
+#pragma unroll
+    for (int i = 1; i < 64; i <<= 1) {
+        low = fmin(low, __shfl_xor(low, i));
+        high = fmax(high, __shfl_xor(high, i));
+    }
+    if ((tid & 63) == 0) {
+        sh_lo[tid >> 6] = low;
+        sh_hi[tid >> 6] = high;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kChooseThreads / 64; ++w) {
+        low = fmin(low, sh_lo[w]);
+        high = fmax(high, sh_hi[w]);
+    }
+    const double scale = high > low ? (kBins - 1) / (high - low) : 0.;
+    // (a range beyond the type's gives scale 0; infinities and NaN lie in the outer bins)
+    auto bin_of = [&](unsigned long long k) {
+        const double x = score_of(k);
+        if (!(x < INFINITY)) return kBins - 1;
+        const double at = (x - low) * scale;
+        return at > 0. ? at < kBins - 1 ? (int)at : kBins - 1 : 0;
+    };
+    for (int i = tid; i < n; i += kChooseThreads) atomicAdd(&bins[bin_of(key(i))], 1);  // whole numbers: any order
+    __syncthreads();
+    find_bin(bins, want, isums, &found);
+    const Found f = found;
     unsigned long long prefix = 0;
     int shift = 64;
+    if (f.count <= kMaxTied) {
+        for (int i = tid; i < n; i += kChooseThreads) {
+            const unsigned long long k = key(i);
+            if (bin_of(k) == f.bin) {
+                const int at = atomicAdd(&sh_n, 1);
+                tied[at] = k;
+                tied_at[at] = i;
+            }
+        }
+        __syncthreads();
+        if (tid < f.count) {
+            const unsigned long long k = tied[tid];
+            const int at = tied_at[tid];
+            int above = 0, before = 0;  // of the bin: higher ones, and equal ones of lower pages
+            for (int i = 0; i < f.count; ++i) {
+                above += tied[i] > k;
+                before += tied[i] == k && tied_at[i] < at;
+            }
+            if (f.above + above + before == want - 1) {  // the last one taken
+                sh_key = k;
+                sh_want = before + 1;
+            }
+        }
+        __syncthreads();
+        prefix = sh_key;
+        want = sh_want;
+        shift = 0;
+    }
+    // scores whose bits from `shift` on are `prefix` are still open; all above it are taken
     while (shift > 0) {
         const int next = max(shift - 11, 0), width = shift - next;
+        __syncthreads();  // the last use of bins and found is over
         for (int i = tid; i < kBins; i += kChooseThreads) bins[i] = 0;
         __syncthreads();
         for (int i = tid; i < n; i += kChooseThreads) {
@@ -150,49 +266,27 @@ __global__ __launch_bounds__(kChooseThreads) void paged_choose_kernel(SelectPara
             if (shift == 64 || k >> shift == prefix) atomicAdd(&bins[(int)(k >> next) & ((1 << width) - 1)], 1);
         }
         __syncthreads();
-        // the highest bin with `want` scores in it and above it: four bins a thread, from the top
-        constexpr int EACH = kBins / kChooseThreads;
-        int mine = 0;
-#pragma unroll
-        for (int i = 0; i < EACH; ++i) mine += bins[kBins - 1 - (tid * EACH + i)];
-        int total;
-        int upto = scan(mine, sums, total);
-        if (upto >= want && upto - mine < want) {
-            int above = upto - mine;
-            for (int i = 0; i < EACH; ++i) {
-                const int bin = kBins - 1 - (tid * EACH + i);
-                if (above + bins[bin] >= want) {
-                    sh_bin = bin;
-                    sh_above = above;
-                    sh_count = bins[bin];
-                    break;
-                }
-                above += bins[bin];
-            }
-        }
-        __syncthreads();
-        prefix = shift == 64 ? (unsigned long long)sh_bin : prefix << width | (unsigned)sh_bin;
-        want -= sh_above;
+        find_bin(bins, want, isums, &found);
+        prefix = shift == 64 ? (unsigned long long)found.bin : prefix << width | (unsigned)found.bin;
+        want -= found.above;
         shift = next;
-        if (sh_count == want) break;
+        if (found.count == want) break;
     }
-    // taken: above the prefix; of those at it, the first `want` (all, unless 64 bits tie)
+    // taken: above the prefix; of those at it, the first `want`.  One scan of both counts.
     const int each = (n + kChooseThreads - 1) / kChooseThreads;
     const int i0 = min(tid * each, n), i1 = min(i0 + each, n);
-    int above = 0, at = 0;
+    long long mine = 0;  // above: low half, at: high half
     for (int i = i0; i < i1; ++i) {
         const unsigned long long k = key(i) >> shift;
-        above += k > prefix;
-        at += k == prefix;
+        mine += k > prefix ? 1 : k == prefix ? 1ll << 32 : 0;
     }
-    int total;
-    const int at_before = scan(at, sums, total) - at;
-    const int taken_at = min(max(want - at_before, 0), at);
-    int to = scan(above + taken_at, sums, total) - (above + taken_at);
-    int left = taken_at;
+    long long total;
+    const long long before = block_scan(mine, sums, total) - mine;
+    int at = (int)(before >> 32);
+    int to = (int)before + min(at, want);
     for (int i = i0; i < i1; ++i) {
         const unsigned long long k = key(i) >> shift;
-        if (k > prefix || (k == prefix && left-- > 0)) out[a.first + to++] = lo + i;
+        if (k > prefix || (k == prefix && at++ < want)) out[a.first + to++] = lo + i;
     }
 }
 
@@ -203,7 +297,7 @@ hipError_t launch_paged_select(const SelectParams& p, hipStream_t stream) {
     const int rows = p.t.B * p.Hkv;
     if (p.t.max_pages > p.S) {
         const int tiles = (p.t.max_pages + kScoreWaves * 16 - 1) / (kScoreWaves * 16);
-        const int most = (2048 + rows - 1) / rows;
+        const int most = (768 + rows - 1) / rows;
         paged_score_kernel<D, T><<<dim3(tiles < most ? tiles : most, rows), kScoreWaves * 64, 0, stream>>>(p);
     }
     paged_choose_kernel<<<rows, kChooseThreads, 0, stream>>>(p);

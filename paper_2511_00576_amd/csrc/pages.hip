@@ -13,36 +13,14 @@ namespace {
 // sequences' numbers of pages: the r-th new page, in the order of (sequence, page),
 // is the r-th from the top, and pages given back are laid down in the reverse
 // order, so that a rollback restores the stack it started from.  One workgroup
-// walks all sequences, 1024 at a time, since every sequence's pages depend on the
-// sum before it; bound by latency (a scan and a handful of dependent loads).
+// walks all sequences, a thread each, since every sequence's pages depend on the
+// sum before it.  Bound by latency (a scan and a handful of dependent loads).
 constexpr int kTableThreads = 1024;
 // Tokens of a sequence whose slots the scanning thread writes by itself (a page holds 16 at
 // least, so they need one new page at most); more go through a launch of their own.
 constexpr int kFewTokens = 16;
 // Slots that a workgroup of that launch writes.
 constexpr int kSlotTile = 1024;
-
-// Inclusive sum over the workgroup; `total` the whole sum.  (64 bits: what is asked
-// for may pass 2^31 pages.)
-__device__ __forceinline__ long long block_scan(long long x, long long* sums, long long& total) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-#pragma unroll
-    for (int i = 1; i < 64; i <<= 1) {
-        const long long y = __shfl_up(x, i);
-        if (lane >= i) x += y;
-    }
-    __syncthreads();  // the last use of sums is over
-    if (lane == 63) sums[wave] = x;
-    __syncthreads();
-    long long before = 0;
-    total = 0;
-    for (int w = 0; w < waves; ++w) {
-        const long long s = sums[w];
-        if (w < wave) before += s;
-        total += s;
-    }
-    return x + before;
-}
 
 __global__ __launch_bounds__(kTableThreads) void page_extend_kernel(PageTableView t, const int* __restrict__ counts, int T,
                                                                     int* __restrict__ slots, int* __restrict__ start,
@@ -52,7 +30,7 @@ __global__ __launch_bounds__(kTableThreads) void page_extend_kernel(PageTableVie
     const int mask = (1 << t.shift) - 1;
     const int n_free = min(max(t.n_free[0], 0), t.n_pages);
     long long carry = 0;
-    for (int b0 = 0; b0 < t.B; b0 += kTableThreads) {
+    for (int b0 = 0; b0 < t.B; b0 += (int)blockDim.x) {
         const int b = b0 + tid;
         int n = 0, c = 0, held = 0;
         if (b < t.B) {
@@ -63,7 +41,7 @@ __global__ __launch_bounds__(kTableThreads) void page_extend_kernel(PageTableVie
         }
         int need = pages_of(n + c, t.shift) - held;
         long long total;
-        const long long upto = carry + block_scan(need, sums, total);
+        const long long upto = carry + block_scan((long long)need, sums, total);  // may pass 2^31
         carry += total;
         // a sequence that the stack does not suffice for gets nothing; what it asked
         // for still counts, so that later ones do not overtake it
@@ -93,7 +71,7 @@ __global__ __launch_bounds__(kTableThreads) void page_extend_kernel(PageTableVie
     if (tid == 0) taken = 0;
     __syncthreads();
     int mine = 0;
-    for (int b = tid; b < t.B; b += kTableThreads)
+    for (int b = tid; b < t.B; b += (int)blockDim.x)
         mine += pages_of(start[b] + granted[b], t.shift) - pages_of(start[b], t.shift);
     if (mine) atomicAdd(&taken, mine);  // whole numbers: any order
     __syncthreads();
@@ -132,15 +110,15 @@ __global__ __launch_bounds__(kTableThreads) void page_truncate_kernel(PageTableV
     const int n_free = min(max(t.n_free[0], 0), t.n_pages);
     // the number of all dropped pages comes first: the stack's new top
     int mine = 0;
-    for (int b = tid; b < t.B; b += kTableThreads) {
+    for (int b = tid; b < t.B; b += (int)blockDim.x) {
         const int n = held_tokens(t, b);
         mine += pages_of(n, t.shift) - pages_of(min(n, max(lens[b], 0)), t.shift);
     }
     long long all;
-    block_scan(mine, sums, all);
+    block_scan((long long)mine, sums, all);
     const int dropped = (int)min(all, (long long)t.n_pages);
     int base = 0;
-    for (int b0 = 0; b0 < t.B; b0 += kTableThreads) {
+    for (int b0 = 0; b0 < t.B; b0 += (int)blockDim.x) {
         const int b = b0 + tid;
         int drop = 0, keep = 0;
         if (b < t.B) {
@@ -151,15 +129,15 @@ __global__ __launch_bounds__(kTableThreads) void page_truncate_kernel(PageTableV
             t.n_tok[b] = m;
         }
         long long total;
-        const long long upto = block_scan(drop, sums, total);
+        const long long upto = block_scan((long long)drop, sums, total);
         if (total == 0) continue;  // the same for the whole workgroup
         last[tid] = (int)upto;
         first[tid] = keep;
         __syncthreads();
         // dropped pages in turn over all threads: rank r lies in the first sequence whose
         // running sum passes it
-        for (int r = tid; r < (int)total; r += kTableThreads) {
-            int lo = 0, hi = kTableThreads - 1;
+        for (int r = tid; r < (int)total; r += (int)blockDim.x) {
+            int lo = 0, hi = (int)blockDim.x - 1;
             while (lo < hi) {
                 const int mid = (lo + hi) >> 1;
                 if (last[mid] > r) hi = mid;
@@ -282,14 +260,17 @@ __global__ __launch_bounds__(kAppendThreads) void paged_append_kernel(PagedAppen
 
 }  // namespace
 
+// A thread per sequence (a barrier of 16 waves costs more than one of four).
+static int table_threads(int B) { return B <= 64 ? 64 : B <= 256 ? 256 : kTableThreads; }
+
 hipError_t launch_page_truncate(const PageTableView& t, const int* lens, hipStream_t stream) {
-    page_truncate_kernel<<<1, kTableThreads, 0, stream>>>(t, lens);
+    page_truncate_kernel<<<1, table_threads(t.B), 0, stream>>>(t, lens);
     return hipGetLastError();
 }
 
 hipError_t launch_page_extend(const PageTableView& t, const int* counts, int T, int* slots, int* start, int* granted,
                               hipStream_t stream) {
-    page_extend_kernel<<<1, kTableThreads, 0, stream>>>(t, counts, T, slots, start, granted);
+    page_extend_kernel<<<1, table_threads(t.B), 0, stream>>>(t, counts, T, slots, start, granted);
     if (T > kFewTokens)
         page_slots_kernel<<<dim3((T + kSlotTile - 1) / kSlotTile, t.B), 256, 0, stream>>>(t, T, slots, start, granted);
     return hipGetLastError();
