@@ -19,10 +19,7 @@ namespace eva {
 namespace {
 
 constexpr float kPagedTau = 8.f;  // log2 units: unscaled weights stay <= 256
-#ifndef NWV
-#define NWV 4
-#endif
-constexpr int kPagedWaves = NWV;
+constexpr int kPagedWaves = 4;
 
 // Pages that a row's query attends, of a sequence of n tokens: all it has, or the
 // first so many of its list.

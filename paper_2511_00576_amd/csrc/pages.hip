@@ -106,6 +106,7 @@ __global__ __launch_bounds__(kTableThreads) void page_truncate_kernel(PageTableV
     __shared__ long long sums[kTableThreads / 64];
     __shared__ int last[kTableThreads];   // pages dropped up to and with a sequence of the batch
     __shared__ int first[kTableThreads];  // a sequence's first dropped page
+    constexpr int EACH = 4;
     const int tid = threadIdx.x;
     const int n_free = min(max(t.n_free[0], 0), t.n_pages);
     // the number of all dropped pages comes first: the stack's new top
@@ -136,17 +137,24 @@ __global__ __launch_bounds__(kTableThreads) void page_truncate_kernel(PageTableV
         __syncthreads();
         // dropped pages in turn over all threads: rank r lies in the first sequence whose
         // running sum passes it
-        for (int r = tid; r < (int)total; r += (int)blockDim.x) {
-            int lo = 0, hi = (int)blockDim.x - 1;
-            while (lo < hi) {
-                const int mid = (lo + hi) >> 1;
-                if (last[mid] > r) hi = mid;
-                else lo = mid + 1;
+        for (int r0 = tid; r0 < (int)total; r0 += EACH * (int)blockDim.x) {
+            // EACH searches side by side, since each is a chain of LDS reads
+            int at[EACH];
+#pragma unroll
+            for (int k = 0; k < EACH; ++k) at[k] = 0;
+            for (int half = (int)blockDim.x / 2; half; half /= 2)
+#pragma unroll
+                for (int k = 0; k < EACH; ++k)
+                    if (last[at[k] + half - 1] <= r0 + k * (int)blockDim.x) at[k] += half;
+#pragma unroll
+            for (int k = 0; k < EACH; ++k) {
+                const int r = r0 + k * (int)blockDim.x, l = at[k];
+                if (r >= (int)total) break;
+                int* entry = t.table + (size_t)(b0 + l) * t.max_pages + first[l] + (r - (l ? last[l - 1] : 0));
+                const int to = n_free + dropped - 1 - (base + r);
+                if (to >= 0 && to < t.n_pages) t.free_pages[to] = *entry;
+                *entry = -1;
             }
-            int* entry = t.table + (size_t)(b0 + lo) * t.max_pages + first[lo] + (r - (lo ? last[lo - 1] : 0));
-            const int at = n_free + dropped - 1 - (base + r);
-            if (at >= 0 && at < t.n_pages) t.free_pages[at] = *entry;
-            *entry = -1;
         }
         base += (int)total;
         __syncthreads();
@@ -162,71 +170,109 @@ __global__ __launch_bounds__(kTableThreads) void page_truncate_kernel(PageTableV
 // its page.  Rows go to their slots; the last row of a page brings the mean of
 // the page's keys, summed in fp32 in one fixed order over the rows as the cache
 // holds them, so that it has the same bits however the tokens came in.
+//
+// Threads hold 16-byte pieces of the rows, a piece's thread by the row's place in the page:
+// keys go from registers to their rows and into the sums; values pass through LDS,
+// from which a lane takes the eight slots of a feature, the tiles' 16 bytes.  Rows
+// without a slot (a shorter sequence's padding) are not read.  Bound by memory for prompts
+// (APPEND_FIGURES), by the chain slot -> row -> store for single tokens.
 constexpr int kAppendThreads = 256;
 
 template <int D, typename T>
 __global__ __launch_bounds__(kAppendThreads) void paged_append_kernel(PagedAppendParams a) {
-    constexpr int EPC = 16 / (int)sizeof(T);  // elements of a 16-byte piece
-    constexpr int CH = D / EPC;               // pieces of a row
-    constexpr int ROWS = 32;                  // rows of values staged at a time
-    __shared__ T tile[ROWS][D + 16 / sizeof(T)];
-    __shared__ int sh_slot[256];
-    __shared__ float part[kAppendThreads / (D / 4)][D];
+    constexpr int EPC = 16 / (int)sizeof(T);       // elements of a piece
+    constexpr int CH = D / EPC;                    // pieces of a row
+    constexpr int RPT = kAppendThreads / CH;       // rows that the threads hold at a time
+    constexpr int ROWS = sizeof(T) == 2 ? 64 : 32; // rows of values staged at a time
+    constexpr int NP = ROWS / RPT;
+    constexpr int PAD = 16 / (int)sizeof(T);
+    __shared__ __attribute__((aligned(16))) T tile[ROWS][D + PAD];
+    __shared__ int sh_slots[2 * 256];
+    static_assert(sizeof(tile) >= RPT * D * sizeof(float), "the sums lie over the tile");
     const int P = 1 << a.shift, mask = P - 1;
     const int kvh = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
     const int* srow = a.slots + (size_t)b * a.T;
     const int n_slots = a.n_pages << a.shift;
-    const int o = srow[0] >= 0 ? srow[0] & mask : 0;
-    const int i0 = max((int)blockIdx.x * P - o, 0), i1 = min((int)blockIdx.x * P - o + P, a.T);
-    const int rows = i1 - i0;
-    if (rows <= 0) return;
-    // slots of the run (P <= 256), -1 for what does not lie in the pool
-    if (tid < rows) {
-        const int s = srow[i0 + tid];
-        sh_slot[tid] = s < n_slots ? s : -1;
+    // slots of all tokens that the run may have, whatever the first one's place is (P <= 256)
+    const int at = (int)blockIdx.x * P - P + tid;
+    const int s0 = srow[0];
+    if (tid < P) {
+        const int lo = at >= 0 && at < a.T ? srow[at] : -1, hi = at + P < a.T ? srow[at + P] : -1;
+        sh_slots[tid] = lo < n_slots ? lo : -1;  // -1: none in the pool
+        sh_slots[P + tid] = hi < n_slots ? hi : -1;
     }
+    const int o = s0 >= 0 ? s0 & mask : 0;
+    const int have = blockIdx.x == 0 ? o : 0;  // rows of the page that there are already
+    const int i0 = blockIdx.x == 0 ? 0 : (int)blockIdx.x * P - o;
+    const int end = min(P, have + a.T - i0);   // places [have, end) are the run's
+    if (end <= have) return;
+    const int* sh_slot = sh_slots + P - o;     // by place in the page
     __syncthreads();
     const size_t src = (((size_t)b * a.Hkv + kvh) * a.T + i0) * D;
     const T* kn = static_cast<const T*>(a.k_new) + src;
     const T* vn = static_cast<const T*>(a.v_new) + src;
     T* kp = static_cast<T*>(a.k);
     T* vp = static_cast<T*>(a.vt);
-    auto page_at = [&](int slot) { return ((size_t)(slot >> a.shift) * a.Hkv + kvh) * ((size_t)P * D); };
+    auto page_at = [&](int s) { return ((size_t)(s >> a.shift) * a.Hkv + kvh) * ((size_t)P * D); };
+    const int my_row = tid / CH, piece = tid % CH * EPC;
 
-    for (int e = tid; e < rows * CH; e += kAppendThreads) {
-        const int r = e / CH, ch = e % CH, s = sh_slot[r];
-        if (s < 0) continue;
-        *reinterpret_cast<u32x4*>(kp + page_at(s) + (size_t)(s & mask) * D + ch * EPC) =
-            *reinterpret_cast<const u32x4*>(kn + (size_t)r * D + ch * EPC);
-    }
-    // values: 32 rows through LDS, then the slots of a feature that share a tile of
-    // eight in one or two 16-byte pieces where all eight are here, else one by one
-    for (int r0 = 0; r0 < rows; r0 += ROWS) {
-        const int nr = min(ROWS, rows - r0);
-        for (int e = tid; e < nr * CH; e += kAppendThreads) {
-            const int r = e / CH, ch = e % CH;
-            *reinterpret_cast<u32x4*>(&tile[r][ch * EPC]) =
-                *reinterpret_cast<const u32x4*>(vn + (size_t)(r0 + r) * D + ch * EPC);
+    float sum[EPC];
+#pragma unroll
+    for (int i = 0; i < EPC; ++i) sum[i] = 0.f;
+    auto add = [&](const u32x4& x) {
+        const T* e = reinterpret_cast<const T*>(&x);
+#pragma unroll
+        for (int i = 0; i < EPC; ++i) sum[i] += to_f32(e[i]);
+    };
+    const int last = sh_slot[end - 1];
+    const bool complete = a.mean && end == P && last >= 0 && (last & mask) == mask;
+    if (complete)  // the page's other rows come first
+        for (int r = my_row; r < have; r += RPT)
+            add(*reinterpret_cast<const u32x4*>(kp + page_at(last) + (size_t)r * D + piece));
+    for (int r0 = have / ROWS * ROWS; r0 < end; r0 += ROWS) {
+        if (sh_slot[max(r0, have)] < 0) break;  // the sequence's tokens end here
+        u32x4 kx[NP], vx[NP];
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+            const int r = r0 + p * RPT + my_row;
+            if (r >= have && r < end && sh_slot[r] >= 0) {
+                kx[p] = *reinterpret_cast<const u32x4*>(kn + (size_t)(r - have) * D + piece);
+                vx[p] = *reinterpret_cast<const u32x4*>(vn + (size_t)(r - have) * D + piece);
+            }
+        }
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+            const int r = r0 + p * RPT + my_row;
+            if (r >= have && r < end && sh_slot[r] >= 0) {
+                const int s = sh_slot[r];
+                *reinterpret_cast<u32x4*>(kp + page_at(s) + (size_t)(s & mask) * D + piece) = kx[p];
+                add(kx[p]);
+                *reinterpret_cast<u32x4*>(&tile[r - r0][piece]) = vx[p];
+            }
         }
         __syncthreads();
-        // rows by tile of eight: the first and the last may be short
-        const int s0 = sh_slot[r0];
-        const int skew = s0 >= 0 ? s0 & 7 : 0;
-        const int groups = (nr + skew + 7) / 8;
-        for (int e = tid; e < groups * D; e += kAppendThreads) {
-            const int f = e % D, gr = e / D;
-            const int ra = max(gr * 8 - skew, 0), rb = min(gr * 8 - skew + 8, nr);
-            const int sa = sh_slot[r0 + ra];
-            const bool whole = rb - ra == 8 && sa >= 0 && (sa & 7) == 0 && sh_slot[r0 + rb - 1] == sa + 7;
+        // 16 lanes take 16 features of a tile of eight places
+        const int g0 = max(have - r0, 0) / 8, g1 = (min(end - r0, ROWS) + 7) / 8;
+        for (int u = tid / 16 + g0 * (D / 16); u < g1 * (D / 16); u += kAppendThreads / 16) {
+            const int t0 = u / (D / 16) * 8, f0 = u % (D / 16) * 16, f = f0 + tid % 16;
+            const int sa = sh_slot[r0 + t0];
+            const bool whole = r0 + t0 >= have && r0 + t0 + 8 <= end && sa >= 0 && (sa & 7) == 0 && sh_slot[r0 + t0 + 7] == sa + 7;
             if (whole) {
-                T w[8];
+                T* dst = vp + page_at(sa) + vt_index<D>(f, sa & mask);
+                if constexpr (sizeof(T) == 2) {
+                    const bf16* from = &tile[t0 + tid % 16 / 4][f0 + tid % 4 * 4];
+                    typedef short shortx8 __attribute__((ext_vector_type(8)));
+                    const shortx4 lo = lds_read_tr16(from), hi = lds_read_tr16(from + 4 * (D + PAD));
+                    *reinterpret_cast<shortx8*>(dst) = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                } else {
+                    float w[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) w[i] = tile[ra + i][f];
-                u32x4* dst = reinterpret_cast<u32x4*>(vp + page_at(sa) + vt_index<D>(f, sa & mask));
-#pragma unroll
-                for (int i = 0; i < (int)sizeof(T) / 2; ++i) dst[i] = reinterpret_cast<const u32x4*>(w)[i];
+                    for (int i = 0; i < 8; ++i) w[i] = tile[t0 + i][f];
+                    *reinterpret_cast<floatx4*>(dst) = floatx4{w[0], w[1], w[2], w[3]};
+                    *reinterpret_cast<floatx4*>(dst + 4) = floatx4{w[4], w[5], w[6], w[7]};
+                }
             } else {
-                for (int r = ra; r < rb; ++r) {
+                for (int r = max(t0, have - r0); r < min(t0 + 8, end - r0); ++r) {
                     const int s = sh_slot[r0 + r];
                     if (s >= 0) vp[page_at(s) + vt_index<D>(f, s & mask)] = tile[r][f];
                 }
@@ -234,43 +280,33 @@ __global__ __launch_bounds__(kAppendThreads) void paged_append_kernel(PagedAppen
         }
         __syncthreads();
     }
-
-    const int end = sh_slot[rows - 1];
-    if (!a.mean || end < 0 || (end & mask) != mask) return;
-    // row r of the page is token r - (P - rows) of the run, or already there
-    constexpr int NP = kAppendThreads / (D / 4);  // partial sums of a feature
-    const int f = tid % (D / 4) * 4, part_i = tid / (D / 4);
-    const int have = P - rows;
-    const T* page = kp + page_at(end);
-    floatx4 sum = {0.f, 0.f, 0.f, 0.f};
-    for (int r = part_i; r < P; r += NP) {
-        const T* x = (r < have ? page + (size_t)r * D : kn + (size_t)(r - have) * D) + f;
+    if (!complete) return;
+    float* part = reinterpret_cast<float*>(&tile[0][0]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sum[i] += to_f32(x[i]);
-    }
-    *reinterpret_cast<floatx4*>(&part[part_i][f]) = sum;
+    for (int i = 0; i < EPC; ++i) part[my_row * D + piece + i] = sum[i];
     __syncthreads();
     if (tid < D) {
         float m = 0.f;
 #pragma unroll
-        for (int i = 0; i < NP; ++i) m += part[i][tid];
-        a.mean[((size_t)(end >> a.shift) * a.Hkv + kvh) * D + tid] = m / (float)P;
+        for (int i = 0; i < RPT; ++i) m += part[i * D + tid];
+        a.mean[((size_t)(last >> a.shift) * a.Hkv + kvh) * D + tid] = m / (float)P;
     }
 }
 
 }  // namespace
 
-// A thread per sequence (a barrier of 16 waves costs more than one of four).
-static int table_threads(int B) { return B <= 64 ? 64 : B <= 256 ? 256 : kTableThreads; }
+// Threads, a power of two: a wave for up to 64 sequences (a barrier of 16 waves costs 1 us more),
+// four where pages are moved.
+static int table_threads(int B, int least) { return B > 64 ? kTableThreads : least; }
 
 hipError_t launch_page_truncate(const PageTableView& t, const int* lens, hipStream_t stream) {
-    page_truncate_kernel<<<1, table_threads(t.B), 0, stream>>>(t, lens);
+    page_truncate_kernel<<<1, table_threads(t.B, 256), 0, stream>>>(t, lens);
     return hipGetLastError();
 }
 
 hipError_t launch_page_extend(const PageTableView& t, const int* counts, int T, int* slots, int* start, int* granted,
                               hipStream_t stream) {
-    page_extend_kernel<<<1, table_threads(t.B), 0, stream>>>(t, counts, T, slots, start, granted);
+    page_extend_kernel<<<1, table_threads(t.B, 64), 0, stream>>>(t, counts, T, slots, start, granted);
     if (T > kFewTokens)
         page_slots_kernel<<<dim3((T + kSlotTile - 1) / kSlotTile, t.B), 256, 0, stream>>>(t, T, slots, start, granted);
     return hipGetLastError();
