@@ -1308,7 +1308,8 @@ int paged_route(PagedRoute& r, const eva_pcache* c, const eva_page_table* t, int
     const long long pages = S > 0 && S < t->max_pages ? S : t->max_pages;
     const int tokens = 16 * eva::paged_blocks(c->d, c->dtype == EVA_F32 ? 4 : 2);
     const long long chunks = (pages * t->P + tokens - 1) / tokens;
-    if (r.rows * chunks > 0x7fffffffLL || r.rows > 0x7fffff) return EVA_ERR_UNSUPPORTED;
+    // (threads of a launch stay below 2^32)
+    if (r.rows * chunks > 0x7fffffffLL || (long long)t->B * c->H > 0xffffff) return EVA_ERR_UNSUPPORTED;
     r.wgs = 0;
     if (chunks > eva::kPagedMinPart) {
         const long long parts = (r.rows * chunks + eva::kPagedMinPart - 1) / eva::kPagedMinPart;
@@ -1358,7 +1359,7 @@ int eva_paged_append(const eva_pcache* cache, const void* k_new, const void* v_n
 }
 
 size_t eva_paged_select_workspace_bytes(const eva_pcache* cache, const eva_page_table* table, int S) {
-    if (check_paged(cache, table) != EVA_OK || S < 1 || S >= table->max_pages) return 0;
+    if (check_paged(cache, table) != EVA_OK || S < 1 || table->max_pages <= eva::kSelectAlone) return 0;
     return (size_t)table->B * cache->H_kv * table->max_pages * sizeof(unsigned long long);
 }
 
@@ -1372,7 +1373,7 @@ int eva_paged_select(const eva_pcache* cache, const eva_page_table* table, const
     const size_t need = eva_paged_select_workspace_bytes(cache, table, S);
     if (need && (!ws || !aligned16(ws))) return EVA_ERR_INVALID;
     if (ws_bytes < need) return EVA_ERR_CAPACITY;
-    const eva::SelectParams p{table_of(table), cache->k_mean, q, pages, static_cast<unsigned long long*>(ws), S, first, last,
+    const eva::SelectParams p{table_of(table), cache->k_mean, q, pages, need ? static_cast<unsigned long long*>(ws) : nullptr, S, first, last,
                               cache->H, cache->H_kv, cache->H / cache->H_kv};
     hipStream_t s = static_cast<hipStream_t>(stream);
     return hip_status(dispatch(cache->d, cache->dtype, [&](auto dd, auto t) {
@@ -1412,6 +1413,8 @@ int eva_paged_decode(const eva_pcache* cache, const eva_page_table* table, const
     p.wgs = (int)r.wgs;
     p.f_unit = eva::FastDiv(cache->H_kv * r.n_hg);
     p.f_hg = eva::FastDiv(r.n_hg);
+    p.f_H = eva::FastDiv(cache->H);
+    p.f_G = eva::FastDiv(p.G);
     p.scale_log2 = (float)(1.4426950408889634 / sqrt((double)cache->d));
     if (r.wgs > 0 && ws && aligned16(ws) && ws_bytes >= eva::paged_ws_bytes(r.rows, r.wgs, cache->d))
         p.ws = static_cast<float*>(ws);

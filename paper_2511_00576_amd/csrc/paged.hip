@@ -279,10 +279,10 @@ __device__ __forceinline__ floatx4 finish(float m, float l, const floatx4& o) {
 
 // Workspace: an int2 for each row (x: -1, or 2 w + s for a row whose first part is share
 // s of workgroup w; y: how many workgroups after w hold the rest), then [wgs][2] shares
-// of [16] maxima, [16] sums, [16][D] weighted values.  Share 0 is that of a part's first row,
+// of 16 columns: maximum, sum, two floats unused, [D] weighted values.  Share 0 is that of a part's first row,
 // share 1 that of its last one.
 template <int D>
-__host__ __device__ constexpr int share_floats() { return 16 * (D + 2); }
+__host__ __device__ constexpr int share_floats() { return 16 * share_col(D); }
 __device__ __forceinline__ float* shares_of(const PagedParams& a) { return a.ws + (a.rows + 1) / 2 * 4; }
 
 template <int D, typename T>
@@ -440,11 +440,9 @@ __global__ __launch_bounds__(kPagedWaves * 64) __attribute__((amdgpu_waves_per_e
             if (whole) {
                 store4(static_cast<T*>(a.o) + ((size_t)b * a.H + h0 + col) * D + f, finish(m, sum, o));
             } else {
-                if (f == 0) {
-                    part_ws[col] = m;
-                    part_ws[16 + col] = sum;
-                }
-                *reinterpret_cast<floatx4*>(part_ws + 32 + col * D + f) = o;
+                float* to = part_ws + col * share_col(D);
+                if (f == 0) *reinterpret_cast<floatx2*>(to) = floatx2{m, sum};
+                *reinterpret_cast<floatx4*>(to + 4 + f) = o;
             }
         }
         if (!a.ws) return;
@@ -466,80 +464,80 @@ __global__ __launch_bounds__(kPagedWaves * 64) __attribute__((amdgpu_waves_per_e
     }
 }
 
-// Joins the shares of rows that more than one workgroup held: a workgroup per row,
-// threads over (share, column, four features), then over LDS.
-constexpr int kJoinThreads = 512;
+// Joins the shares of rows that more than one workgroup held: a workgroup per query
+// head (one per row would read all its columns through one CU: JOIN_FIGURES), threads
+// over (share, four features), then over LDS.
+constexpr int kJoinThreads = 256;
 template <int D, typename T>
 __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedParams a) {
-    __shared__ float red_m[kJoinThreads], red_l[kJoinThreads];
-    __shared__ __attribute__((aligned(16))) floatx4 red_o[kJoinThreads];
-    const int row = blockIdx.x;
-    const int b = row / a.f_unit;
+    constexpr int ITEMS = D / 4, GROUPS = kJoinThreads / ITEMS;
+    constexpr int NB = 4;  // shares whose loads are in flight together
+    __shared__ float red_m[GROUPS], red_l[GROUPS];
+    __shared__ __attribute__((aligned(16))) floatx4 red_o[GROUPS][ITEMS];
+    const int b = (int)blockIdx.x / a.f_H, h = (int)blockIdx.x % a.f_H;
     if (a.active && a.active[b] == 0) return;  // no one has written its entry
-    const int2 info = reinterpret_cast<const int2*>(a.ws)[row];
+    const int kvh = h / a.f_G, hg = h % a.f_G / 16, col = h % a.f_G % 16;
+    const int2 info = reinterpret_cast<const int2*>(a.ws)[b * a.f_unit.d + kvh * a.n_hg + hg];
     if (info.x < 0) return;
-    const int kvh = row % a.f_unit / a.f_hg, hg = row % a.f_unit % a.f_hg;
-    const int ncols = min(16, a.G - hg * 16);
     const int shares = 1 + info.y;
     const float* first = shares_of(a) + (size_t)info.x * share_floats<D>();
     const float* rest = shares_of(a) + (size_t)((info.x >> 1) + 1) * 2 * share_floats<D>();
-    const int items = ncols * (D / 4);  // 16 .. 512
-    constexpr int NB = 8;  // shares whose loads are in flight together
-    const int groups = min(kJoinThreads / items, (shares + NB - 1) / NB);
-    const int grp = threadIdx.x / items, e = threadIdx.x % items;
-    const int col = e / (D / 4), f = e % (D / 4) * 4;
+    const int grp = threadIdx.x / ITEMS, f = threadIdx.x % ITEMS * 4;
     float M = -INFINITY, L = 0.f;
     floatx4 O = {0.f, 0.f, 0.f, 0.f};
-    if (grp < groups) {
-        for (int s0 = grp; s0 < shares; s0 += groups * NB) {
-            float m[NB], l[NB];
-            floatx4 o[NB];
+    for (int s0 = grp; s0 < shares; s0 += GROUPS * NB) {
+        float m[NB], l[NB];
+        floatx4 o[NB];
 #pragma unroll
-            for (int i = 0; i < NB; ++i) {
-                const int s = min(s0 + i * groups, shares - 1);
-                const float* w = s == 0 ? first : rest + (size_t)(s - 1) * 2 * share_floats<D>();
-                m[i] = w[col];
-                l[i] = w[16 + col];
-                o[i] = *reinterpret_cast<const floatx4*>(w + 32 + col * D + f);
-            }
-            float top = M;
-#pragma unroll
-            for (int i = 0; i < NB; ++i) {
-                if (s0 + i * groups >= shares) {  // past the last
-                    m[i] = -INFINITY;
-                    l[i] = 0.f;
-                    o[i] = floatx4{0.f, 0.f, 0.f, 0.f};
-                }
-                top = fmaxf(top, m[i]);
-            }
-            const float keep = top == -INFINITY ? 1.f : M == -INFINITY ? 0.f : fast_exp2(M - top);
-            L *= keep;
-            O *= keep;
-#pragma unroll
-            for (int i = 0; i < NB; ++i) {
-                const float wt = top == -INFINITY ? 1.f : m[i] == -INFINITY ? 0.f : fast_exp2(m[i] - top);
-                L += wt * l[i];
-                O += wt * o[i];
-            }
-            M = top;
+        for (int i = 0; i < NB; ++i) {
+            const int s = min(s0 + i * GROUPS, shares - 1);
+            const float* w = (s == 0 ? first : rest + (size_t)(s - 1) * 2 * share_floats<D>()) + col * share_col(D);
+            const floatx2 ml = *reinterpret_cast<const floatx2*>(w);
+            m[i] = ml[0];
+            l[i] = ml[1];
+            o[i] = *reinterpret_cast<const floatx4*>(w + 4 + f);
         }
+        float top = M;
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+            if (s0 + i * GROUPS >= shares) {  // past the last
+                m[i] = -INFINITY;
+                l[i] = 0.f;
+                o[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+            }
+            top = fmaxf(top, m[i]);
+        }
+        const float keep = top == -INFINITY ? 1.f : M == -INFINITY ? 0.f : fast_exp2(M - top);
+        L *= keep;
+        O *= keep;
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+            const float wt = top == -INFINITY ? 1.f : m[i] == -INFINITY ? 0.f : fast_exp2(m[i] - top);
+            L += wt * l[i];
+            O += wt * o[i];
+        }
+        M = top;
     }
-    red_m[threadIdx.x] = M;
-    red_l[threadIdx.x] = L;
-    red_o[threadIdx.x] = O;
+    if (f == 0) {
+        red_m[grp] = M;
+        red_l[grp] = L;
+    }
+    red_o[grp][f / 4] = O;
     __syncthreads();
     if (grp != 0) return;
     float top = M;
-    for (int i = 1; i < groups; ++i) top = fmaxf(top, red_m[i * items + e]);
+#pragma unroll
+    for (int i = 1; i < GROUPS; ++i) top = fmaxf(top, red_m[i]);
     float sum = 0.f;
     floatx4 out = {0.f, 0.f, 0.f, 0.f};
-    for (int i = 0; i < groups; ++i) {
-        const float m = red_m[i * items + e];
+#pragma unroll
+    for (int i = 0; i < GROUPS; ++i) {
+        const float m = red_m[i];
         const float wt = top == -INFINITY ? 1.f : m == -INFINITY ? 0.f : fast_exp2(m - top);
-        sum += wt * red_l[i * items + e];
-        out += wt * red_o[i * items + e];
+        sum += wt * red_l[i];
+        out += wt * red_o[i][f / 4];
     }
-    store4(static_cast<T*>(a.o) + ((size_t)b * a.H + kvh * a.G + hg * 16 + col) * D + f, finish(top, sum, out));
+    store4(static_cast<T*>(a.o) + (size_t)blockIdx.x * D + f, finish(top, sum, out));
 }
 
 }  // namespace
@@ -547,7 +545,7 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedParams a)
 template <int D, typename T>
 hipError_t launch_paged_decode(const PagedParams& p, hipStream_t stream) {
     paged_decode_kernel<D, T><<<p.ws ? p.wgs : p.rows, kPagedWaves * 64, 0, stream>>>(p);
-    if (p.ws) paged_join_kernel<D, T><<<p.rows, kJoinThreads, 0, stream>>>(p);
+    if (p.ws) paged_join_kernel<D, T><<<p.t.B * p.H, kJoinThreads, 0, stream>>>(p);
     return hipGetLastError();
 }
 template hipError_t launch_paged_decode<64, bf16>(const PagedParams&, hipStream_t);

@@ -101,6 +101,7 @@ struct PagedParams {
     int rows;           // B Hkv n_hg
     int wgs;            // workgroups that share all rows' chunks (with ws)
     FastDiv f_unit, f_hg;  // divisors of Hkv n_hg and of n_hg
+    FastDiv f_H, f_G;      // of H and of G
     float scale_log2;
 };
 // Blocks of 16 tokens in a chunk, what a wave requests at once: 16 KB of keys and
@@ -110,9 +111,11 @@ constexpr int paged_blocks(int d, int bytes) { return bytes == 4 && d == 128 ? 1
 constexpr int kPagedMinPart = 4;
 // Workgroups that share a decode's chunks: as many as the CUs hold at once.
 constexpr int kPagedWgs = 512;
+// Floats of a column of a share (paged.hip).
+__host__ __device__ constexpr int share_col(int d) { return d + 4; }
 // Bytes of the workspace: a pair of ints per row, then two shares per workgroup.
 inline size_t paged_ws_bytes(long long rows, long long wgs, int d) {
-    return ((size_t)(rows + 1) / 2 * 4 + (size_t)wgs * 2 * 16 * (d + 2)) * sizeof(float);
+    return ((size_t)(rows + 1) / 2 * 4 + (size_t)wgs * 2 * 16 * share_col(d)) * sizeof(float);
 }
 template <int D, typename T>
 hipError_t launch_paged_decode(const PagedParams& p, hipStream_t stream);
@@ -122,9 +125,12 @@ struct SelectParams {
     const float* mean;  // [n_pages][Hkv][d]
     const void* q;      // [B][H][d]
     int* pages;         // [B][Hkv][S]
-    unsigned long long* keys;  // [B Hkv][max_pages]: scores as ordered whole numbers
+    unsigned long long* keys;  // [B Hkv][max_pages]: scores as ordered whole numbers; nullptr: in LDS
     int S, first, last, H, Hkv, G;
 };
+// The most pages of a table's row for which the workgroup that chooses makes the scores
+// itself.
+constexpr int kSelectAlone = 1024;
 template <int D, typename T>
 hipError_t launch_paged_select(const SelectParams& p, hipStream_t stream);
 

@@ -17,6 +17,7 @@ constexpr int kScoreWaves = 4;
 constexpr int kChooseThreads = 512;
 // Scores held in LDS by the choosing workgroup; longer rows are read again from memory.
 constexpr int kChooseLds = 4096;
+static_assert(kSelectAlone <= kChooseLds, "scores made by the choosing workgroup stay in LDS");
 constexpr int kBins = 2048;  // 11 bits a pass
 // Scores of the bin in which the choice ends that are ranked one against the other.
 constexpr int kMaxTied = 256;
@@ -30,9 +31,18 @@ __device__ __forceinline__ unsigned long long ordered(double x) {
     return u >> 63 ? ~u : u | 1ull << 63;
 }
 
-// The score again; bits that no score has (NaN) stay one.
-__device__ __forceinline__ double score_of(unsigned long long k) {
-    return __builtin_bit_cast(double, k >> 63 ? k & ~(1ull << 63) : ~k);
+// The score again, in 32 bits; a NaN stays one.
+__device__ __forceinline__ float score_of(unsigned long long k) {
+    return (float)__builtin_bit_cast(double, k >> 63 ? k & ~(1ull << 63) : ~k);
+}
+
+// Largest over the wave, in every lane.
+__device__ __forceinline__ float wave_max(float x) {
+    x = fmaxf(x, __builtin_bit_cast(float, dpp<0xb1>(__builtin_bit_cast(int, x))));   // lanes 1 0 3 2 of a quad
+    x = fmaxf(x, __builtin_bit_cast(float, dpp<0x4e>(__builtin_bit_cast(int, x))));   // 2 3 0 1
+    x = fmaxf(x, __builtin_bit_cast(float, dpp<0x124>(__builtin_bit_cast(int, x))));  // a row of 16 turned by four
+    x = fmaxf(x, __builtin_bit_cast(float, dpp<0x128>(__builtin_bit_cast(int, x))));  // by eight
+    return xgroup_max(x);
 }
 
 __device__ __forceinline__ void load4(const float* p, float (&x)[4]) {
@@ -46,28 +56,24 @@ __device__ __forceinline__ void load4(const bf16* p, float (&x)[4]) {
     for (int i = 0; i < 4; ++i) x[i] = (float)v[i];
 }
 
-// Pages of sequence b that are ranked: [lo, hi).  None where all are kept.
-__device__ __forceinline__ void ranked(const SelectParams& a, int held, int& lo, int& hi) {
-    lo = hi = 0;
-    if (held > a.S) {
-        lo = a.first;
-        hi = held - a.last;
-    }
+// How many pages of a sequence are ranked, those from a.first on; none where all are
+// kept.
+__device__ __forceinline__ int ranked(const SelectParams& a, int held) {
+    return held > a.S ? held - a.first - a.last : 0;
 }
 
-// One wave scores 16 pages for four query heads at a time, with the matrix core's four
+// A wave scores 16 pages for four query heads at a time, with the matrix core's four
 // products of 4 x 4 x 4: block c / 4 holds pages 4 (c / 4) + 0 .. 3 and all four the same heads,
 //     A lane (g, c): page c, B: head c % 4, both contraction index g, which is feature
 //     16 i + 4 g + e in step (i, e), so that the mean keys are 16-byte loads;
 //     D lane (g, c): page 4 (c / 4) + g, head c % 4.
 // (The 16 x 16 x 4 product, at the same rate, would spend three quarters of its columns on
-// heads that there are not: 22 us against 11 us for 256 rows of 513 pages, d = 128.)
-// Bound by the mean keys' read and the chain count -> table -> mean.
-template <int D, typename T>
-__global__ __launch_bounds__(kScoreWaves * 64) void paged_score_kernel(SelectParams a) {
-    const int b = (int)blockIdx.y / a.Hkv, kvh = (int)blockIdx.y % a.Hkv;
-    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int g = lane >> 4, c = lane & 15;
+// heads that there are not: 22 us against 11 for 256 rows of 513 pages, d = 128.)
+// Scores 16 (tile + k tiles) + 0 .. 15 of the row go to put(index, score).  Returns how many
+// pages are ranked.
+template <int D, typename T, typename Put>
+__device__ __forceinline__ int score_pages(const SelectParams& a, int b, int kvh, int tile, int tiles, Put put) {
+    const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
     const T* heads = static_cast<const T*>(a.q) + ((size_t)b * a.H + (size_t)kvh * a.G) * D + 4 * g;
     // the heads h0 .. h0 + 3; past the last they repeat it, which changes no maximum
     double q[D / 4];
@@ -81,25 +87,21 @@ __global__ __launch_bounds__(kScoreWaves * 64) void paged_score_kernel(SelectPar
             for (int e = 0; e < 4; ++e) q[4 * i + e] = (double)x[e];
         }
     };
-    const int step = gridDim.x * kScoreWaves * 16;
-    int j0 = ((int)blockIdx.x * kScoreWaves + wave) * 16;  // from the first ranked page on
     // a tile's pages are looked up one tile ahead, the first before the sequence's length is
     // known (any entry of its row may be read; what it names is checked below)
     const int* row = a.t.table + (size_t)b * a.t.max_pages;
     auto look_up = [&](int j) { return row[min(a.first + j + c, a.t.max_pages - 1)]; };
-    int next = look_up(j0);
+    int j0 = tile * 16, next = look_up(j0);
     load_heads(0);
-    const int held = pages_of(held_tokens(a.t, b), a.t.shift);
-    int lo, hi;
-    ranked(a, held, lo, hi);
-    for (; j0 < hi - lo; j0 += step) {
-        const int page = next;
+    const int n = ranked(a, pages_of(held_tokens(a.t, b), a.t.shift));
+    for (; j0 < n; j0 += tiles * 16) {
+        const int page = next;  // past the last ranked page: others, whose scores are not used
         const bool lost = (unsigned)page >= (unsigned)a.t.n_pages;
         const float* mean = a.mean + ((size_t)(lost ? 0 : page) * a.Hkv + kvh) * D + 4 * g;
         floatx4 m[D / 16];
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) m[i] = *reinterpret_cast<const floatx4*>(mean + 16 * i);
-        if (j0 + step < hi - lo) next = look_up(j0 + step);
+        if (j0 + tiles * 16 < n) next = look_up(j0 + tiles * 16);
         const unsigned long long lost_rows = __builtin_amdgcn_ballot_w64(lost);
         unsigned long long best = 0;
         for (int h0 = 0; h0 < a.G; h0 += 4) {
@@ -119,9 +121,19 @@ __global__ __launch_bounds__(kScoreWaves * 64) void paged_score_kernel(SelectPar
         best = other > best ? other : best;
         const int j = (c & 12) + g;
         // a page that the pool does not have ranks first: its row becomes NaN
-        if ((c & 3) == 0 && j0 + j < hi - lo)
-            a.keys[(size_t)blockIdx.y * a.t.max_pages + j0 + j] = lost_rows >> j & 1 ? ~0ull : best;
+        if ((c & 3) == 0 && j0 + j < n) put(j0 + j, lost_rows >> j & 1 ? ~0ull : best);
     }
+    return n;
+}
+
+// Bound by the mean keys' read and the chain table -> mean.
+template <int D, typename T>
+__global__ __launch_bounds__(kScoreWaves * 64) void paged_score_kernel(SelectParams a) {
+    const int b = (int)blockIdx.y / a.Hkv, kvh = (int)blockIdx.y % a.Hkv;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    unsigned long long* keys = a.keys + (size_t)blockIdx.y * a.t.max_pages;
+    score_pages<D, T>(a, b, kvh, (int)blockIdx.x * kScoreWaves + wave, (int)gridDim.x * kScoreWaves,
+                      [&](int j, unsigned long long k) { keys[j] = k; });
 }
 
 // Of a workgroup's bins, the one in which the `want`-th highest score lies: each thread
@@ -151,16 +163,17 @@ __device__ __forceinline__ void find_bin(const int* bins, int want, int* sums, F
 }
 
 // A workgroup per (sequence, kv head).  The scores are counted in bins of equal width
-// between the lowest and the highest (a map that keeps their order), which spreads them; the
-// `want`-th highest lies in one bin, whose few scores are ranked one against the other.
-// Where it holds many (scores that tie, or one far from all others), a radix search
-// over the bits finds it instead, 11 a pass.  Then the pages in their order.  Bound by
-// the passes' barriers.
+// between the lowest and the highest (a map that keeps their order, in 32 bits), which
+// spreads them; the `want`-th highest lies in one bin, whose few scores are ranked one
+// against the other.  Where it holds many (scores that tie, or one far from all others), a
+// radix search over the bits finds it instead, 11 a pass.  Then the pages in their order.
+// Bound by the passes' barriers.  SCORE: the workgroup makes the scores first, in LDS.
+template <int D, typename T, bool SCORE>
 __global__ __launch_bounds__(kChooseThreads) void paged_choose_kernel(SelectParams a) {
     __shared__ unsigned long long sh_keys[kChooseLds];
     __shared__ int bins[kBins];
     __shared__ long long sums[kChooseThreads / 64];
-    __shared__ double sh_lo[kChooseThreads / 64], sh_hi[kChooseThreads / 64];
+    __shared__ float sh_lo[kChooseThreads / 64], sh_hi[kChooseThreads / 64];
     __shared__ unsigned long long tied[kMaxTied];
     __shared__ int tied_at[kMaxTied];
     __shared__ Found found;
@@ -168,9 +181,16 @@ __global__ __launch_bounds__(kChooseThreads) void paged_choose_kernel(SelectPara
     __shared__ unsigned long long sh_key;
     int* isums = reinterpret_cast<int*>(sums);
     const int b = (int)blockIdx.x / a.Hkv, tid = threadIdx.x;
+    const unsigned long long* gkeys = a.keys + (size_t)blockIdx.x * a.t.max_pages;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    for (int i = tid; i < kBins; i += kChooseThreads) bins[i] = 0;
+    if (tid == 0) sh_n = 0;
+    if constexpr (SCORE) {
+        score_pages<D, T>(a, b, (int)blockIdx.x % a.Hkv, wave, kChooseThreads / 64,
+                          [&](int j, unsigned long long k) { sh_keys[j] = k; });
+        __syncthreads();
+    }
     const int held = pages_of(held_tokens(a.t, b), a.t.shift);
-    int lo, hi;
-    ranked(a, held, lo, hi);
     int* out = a.pages + (size_t)blockIdx.x * a.S;
     if (held <= a.S) {  // all of them
         for (int i = tid; i < a.S; i += kChooseThreads) out[i] = i < held ? i : -1;
@@ -178,48 +198,42 @@ __global__ __launch_bounds__(kChooseThreads) void paged_choose_kernel(SelectPara
     }
     for (int i = tid; i < a.first; i += kChooseThreads) out[i] = i;
     for (int i = tid; i < a.last; i += kChooseThreads) out[a.S - a.last + i] = held - a.last + i;
-    const int n = hi - lo;
+    const int n = ranked(a, held);
     int want = a.S - a.first - a.last;
     if (want == 0) return;
-    const unsigned long long* gkeys = a.keys + (size_t)blockIdx.x * a.t.max_pages;
-    const bool in_lds = n <= kChooseLds;
+    const bool in_lds = SCORE || n <= kChooseLds;
     auto key = [&](int i) { return in_lds ? sh_keys[i] : gkeys[i]; };
 
     // the finite scores' range
-    double low = INFINITY, high = -INFINITY;
+    float low = INFINITY, high = -INFINITY;
     for (int i = tid; i < n; i += kChooseThreads) {
-        const unsigned long long k = gkeys[i];
-        if (in_lds) sh_keys[i] = k;
-        const double x = score_of(k);
-        if (__builtin_fabs(x) < INFINITY) {
-            low = fmin(low, x);
-            high = fmax(high, x);
+        const unsigned long long k = SCORE ? sh_keys[i] : gkeys[i];
+        if (!SCORE && in_lds) sh_keys[i] = k;
+        const float x = score_of(k);
+        if (fabsf(x) < INFINITY) {
+            low = fminf(low, x);
+            high = fmaxf(high, x);
         }
     }
-    for (int i = tid; i < kBins; i += kChooseThreads) bins[i] = 0;
-    if (tid == 0) sh_n = 0;
-#pragma unroll
-    for (int i = 1; i < 64; i <<= 1) {
-        low = fmin(low, __shfl_xor(low, i));
-        high = fmax(high, __shfl_xor(high, i));
-    }
+    low = -wave_max(-low);
+    high = wave_max(high);
     if ((tid & 63) == 0) {
-        sh_lo[tid >> 6] = low;
-        sh_hi[tid >> 6] = high;
+        sh_lo[wave] = low;
+        sh_hi[wave] = high;
     }
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < kChooseThreads / 64; ++w) {
-        low = fmin(low, sh_lo[w]);
-        high = fmax(high, sh_hi[w]);
+        low = fminf(low, sh_lo[w]);
+        high = fmaxf(high, sh_hi[w]);
     }
-    const double scale = high > low ? (kBins - 1) / (high - low) : 0.;
+    const float scale = high > low ? (kBins - 1) / (high - low) : 0.f;
     // (a range beyond the type's gives scale 0; infinities and NaN lie in the outer bins)
     auto bin_of = [&](unsigned long long k) {
-        const double x = score_of(k);
+        const float x = score_of(k);
         if (!(x < INFINITY)) return kBins - 1;
-        const double at = (x - low) * scale;
-        return at > 0. ? at < kBins - 1 ? (int)at : kBins - 1 : 0;
+        const float at = (x - low) * scale;
+        return at > 0.f ? at < kBins - 1 ? (int)at : kBins - 1 : 0;
     };
     for (int i = tid; i < n; i += kChooseThreads) atomicAdd(&bins[bin_of(key(i))], 1);  // whole numbers: any order
     __syncthreads();
@@ -286,7 +300,7 @@ __global__ __launch_bounds__(kChooseThreads) void paged_choose_kernel(SelectPara
     int to = (int)before + min(at, want);
     for (int i = i0; i < i1; ++i) {
         const unsigned long long k = key(i) >> shift;
-        if (k > prefix || (k == prefix && at++ < want)) out[a.first + to++] = lo + i;
+        if (k > prefix || (k == prefix && at++ < want)) out[a.first + to++] = a.first + i;
     }
 }
 
@@ -295,12 +309,14 @@ __global__ __launch_bounds__(kChooseThreads) void paged_choose_kernel(SelectPara
 template <int D, typename T>
 hipError_t launch_paged_select(const SelectParams& p, hipStream_t stream) {
     const int rows = p.t.B * p.Hkv;
-    if (p.t.max_pages > p.S) {
-        const int tiles = (p.t.max_pages + kScoreWaves * 16 - 1) / (kScoreWaves * 16);
-        const int most = (768 + rows - 1) / rows;
-        paged_score_kernel<D, T><<<dim3(tiles < most ? tiles : most, rows), kScoreWaves * 64, 0, stream>>>(p);
+    if (!p.keys) {
+        paged_choose_kernel<D, T, true><<<rows, kChooseThreads, 0, stream>>>(p);
+        return hipGetLastError();
     }
-    paged_choose_kernel<<<rows, kChooseThreads, 0, stream>>>(p);
+    const int tiles = (p.t.max_pages + kScoreWaves * 16 - 1) / (kScoreWaves * 16);
+    const int most = (768 + rows - 1) / rows;  // as many as the CUs hold at once
+    paged_score_kernel<D, T><<<dim3(tiles < most ? tiles : most, rows), kScoreWaves * 64, 0, stream>>>(p);
+    paged_choose_kernel<D, T, false><<<rows, kChooseThreads, 0, stream>>>(p);
     return hipGetLastError();
 }
 template hipError_t launch_paged_select<64, bf16>(const SelectParams&, hipStream_t);

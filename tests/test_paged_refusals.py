@@ -55,6 +55,7 @@ def select(lib, c=None, t=None, q=FAKE, S=5, first=1, last=1, pages=FAKE, ws=FAK
     return lib.eva_paged_select(ref(c or pool()), ref(t or table()), q, S, first, last, pages, ws, n, None)
 
 
+LONG = table(max_pages=2000)  # more pages a sequence than one workgroup scores and ranks
 TABLES = [(dict(B=0), INVALID), (dict(P=0), INVALID), (dict(P=8), INVALID), (dict(P=48), INVALID), (dict(P=512), INVALID),
           (dict(n_pages=0), INVALID), (dict(max_pages=0), INVALID), (dict(n_tok=None), INVALID), (dict(table=0x60002), INVALID),
           (dict(free_pages=None), INVALID), (dict(n_free=0x80001), INVALID), (dict(n_pages=2 ** 24 + 1), UNSUPPORTED),
@@ -105,8 +106,9 @@ def test_null_structs(lib):
     (decode, dict(c=pool(H=60000, H_kv=30000), t=table(max_pages=2 ** 24)), UNSUPPORTED),  # chunks of all rows
     (select, dict(S=0), INVALID), (select, dict(first=-1), INVALID), (select, dict(last=0), INVALID),
     (select, dict(first=4, last=2), INVALID), (select, dict(q=None), INVALID), (select, dict(pages=OFF2), INVALID),
-    (select, dict(c=pool(k_mean=None)), INVALID), (select, dict(ws=None), INVALID), (select, dict(ws=OFF8), INVALID),
-    (select, dict(n=2 * 2 * 40 * 8 - 1), CAPACITY), (select, dict(t=table(P=32)), INVALID),
+    (select, dict(c=pool(k_mean=None)), INVALID), (select, dict(t=table(P=32)), INVALID),
+    (select, dict(t=LONG, ws=None), INVALID), (select, dict(t=LONG, ws=OFF8), INVALID),
+    (select, dict(t=LONG, n=2 * 2 * 2000 * 8 - 1), CAPACITY),
 ])
 def test_calls_are_checked(lib, call, kw, code):
     assert call(lib, **kw) == code
@@ -114,8 +116,8 @@ def test_calls_are_checked(lib, call, kw, code):
 
 def test_workspaces(lib):
     c, t = pool(), table()
-    assert lib.eva_paged_select_workspace_bytes(ref(c), ref(t), 5) == 2 * 2 * 40 * 8
-    assert lib.eva_paged_select_workspace_bytes(ref(c), ref(t), 40) == 0      # all pages are kept
+    assert lib.eva_paged_select_workspace_bytes(ref(c), ref(LONG), 5) == 2 * 2 * 2000 * 8
+    assert lib.eva_paged_select_workspace_bytes(ref(c), ref(t), 5) == 0
     assert lib.eva_paged_decode_workspace_bytes(ref(c), ref(t), 0) > 0
     assert lib.eva_paged_decode_workspace_bytes(ref(c), ref(t), 1) == 0       # two chunks a row: one workgroup each
     assert lib.eva_paged_decode_workspace_bytes(ref(c), ref(t), -1) == 0
