@@ -1359,7 +1359,8 @@ int eva_paged_append(const eva_pcache* cache, const void* k_new, const void* v_n
 }
 
 size_t eva_paged_select_workspace_bytes(const eva_pcache* cache, const eva_page_table* table, int S) {
-    if (check_paged(cache, table) != EVA_OK || S < 1 || table->max_pages <= eva::kSelectAlone) return 0;
+    if (check_paged(cache, table) != EVA_OK || S < 1 || eva::select_alone((long long)table->B * cache->H_kv, table->max_pages))
+        return 0;
     return (size_t)table->B * cache->H_kv * table->max_pages * sizeof(unsigned long long);
 }
 

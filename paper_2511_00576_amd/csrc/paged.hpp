@@ -128,9 +128,19 @@ struct SelectParams {
     unsigned long long* keys;  // [B Hkv][max_pages]: scores as ordered whole numbers; nullptr: in LDS
     int S, first, last, H, Hkv, G;
 };
-// The most pages of a table's row for which the workgroup that chooses makes the scores
-// itself.
-constexpr int kSelectAlone = 1024;
+// Whether the workgroup that chooses makes its row's scores itself, in LDS, or a launch before
+// spreads them over the chip: one CU reads 35 GB/s of mean keys, so many pages of few rows
+// want more of them.  us in a replayed graph, alone / spread, d = 128 (a call that is not
+// captured pays 2.6 us of host time for the second launch, so the bound is 256 and not 128):
+//     rows   128 pages   256          512          1024         2048
+//        8   8.4 / 8.8   10.2 / 8.8   13.9 / 9.0   21 / 10      36 / 12
+//      128   8.6 / 9.0   10.5 / 10.7  14.9 / 15.2  22 / 22      37 / 34
+//      256   8.6 / 10.7  11.0 / 15.1  18 / 21      29 / 33      50 / 57
+//      512   16 / 16     21 / 22      33 / 35      53 / 63      113 / 143
+constexpr int kSelectAlone = 4096;  // scores that LDS holds
+inline bool select_alone(long long rows, int max_pages) {
+    return max_pages <= 256 || (rows >= 256 && max_pages <= kSelectAlone);
+}
 template <int D, typename T>
 hipError_t launch_paged_select(const SelectParams& p, hipStream_t stream);
 

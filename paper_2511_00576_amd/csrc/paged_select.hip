@@ -16,8 +16,7 @@ namespace {
 constexpr int kScoreWaves = 4;
 constexpr int kChooseThreads = 512;
 // Scores held in LDS by the choosing workgroup; longer rows are read again from memory.
-constexpr int kChooseLds = 4096;
-static_assert(kSelectAlone <= kChooseLds, "scores made by the choosing workgroup stay in LDS");
+constexpr int kChooseLds = kSelectAlone;
 constexpr int kBins = 2048;  // 11 bits a pass
 // Scores of the bin in which the choice ends that are ranked one against the other.
 constexpr int kMaxTied = 256;
@@ -106,13 +105,13 @@ __device__ __forceinline__ int score_pages(const SelectParams& a, int b, int kvh
         unsigned long long best = 0;
         for (int h0 = 0; h0 < a.G; h0 += 4) {
             if (a.G > 4) load_heads(h0);
-            double acc = 0.;
+            double acc[4] = {0., 0., 0., 0.};  // four chains of products that wait for each other
 #pragma unroll
             for (int i = 0; i < D / 16; ++i)
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    acc = __builtin_amdgcn_mfma_f64_4x4x4f64((double)m[i][e], q[4 * i + e], acc, 0, 0, 0);
-            const unsigned long long k = ordered(acc);
+                    acc[e] = __builtin_amdgcn_mfma_f64_4x4x4f64((double)m[i][e], q[4 * i + e], acc[e], 0, 0, 0);
+            const unsigned long long k = ordered((acc[0] + acc[1]) + (acc[2] + acc[3]));
             best = k > best ? k : best;
         }
         unsigned long long other = (unsigned long long)dpp<0xb1>((long long)best);  // lanes 1 0 3 2 of a quad
