@@ -726,7 +726,7 @@ typedef struct eva_page_table {
  *     start[b]    = n, the position of the first one (eva_qk_norm_rope's `start`)
  * slots [B][T], start, granted [B]: device int32.  Nothing else is changed.
  * Errors: INVALID (malformed table, T < 1, null or misaligned pointers),
- * UNSUPPORTED (sizes, T above 2^30).
+ * UNSUPPORTED (sizes, T above 2^30, B ceil(T / 1024) above 2^24).
  */
 int eva_page_extend(const eva_page_table* table, const int* counts, int T, int* slots, int* start, int* granted,
                     void* stream);
@@ -782,6 +782,7 @@ int eva_paged_append(const eva_pcache* cache, const void* k_new, const void* v_n
  * often as it stands there (entries that are none of the sequence's pages: nothing).
  * A row without keys is zeros.  Rows of sequences that are not active (device int32 [B], 0; NULL: all are)
  * are left as they were.  A row that meets an entry of the table outside the pool is NaN.
+ * o may not overlap q.
  * ws: optional device scratch of eva_paged_decode_workspace_bytes() bytes, which
  * every call that overlaps another needs for its own: the chunks of 32 tokens of all
  * rows are shared evenly by the workgroups, and rows that several of them had are

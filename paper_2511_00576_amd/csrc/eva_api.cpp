@@ -1336,7 +1336,8 @@ int eva_page_extend(const eva_page_table* table, const int* counts, int T, int* 
     if (T < 1 || !slots || !start || !granted || !aligned4(counts) || !aligned4(slots) || !aligned4(start) ||
         !aligned4(granted))
         return EVA_ERR_INVALID;
-    if (T > kMaxLen) return EVA_ERR_UNSUPPORTED;
+    // threads of a launch stay below 2^32
+    if (T > kMaxLen || (long long)((T + 1023) / 1024) * table->B > 0xffffff) return EVA_ERR_UNSUPPORTED;
     return hip_status(eva::launch_page_extend(table_of(table), counts, T, slots, start, granted,
                                               static_cast<hipStream_t>(stream)));
 }

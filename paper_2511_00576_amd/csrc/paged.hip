@@ -68,8 +68,8 @@ __device__ __forceinline__ void locate(Block (&x)[NB], const PagedParams& a, int
         if (e < n_pages) {
             int lp = e;
             if (a.pages) lp = scalar_load(a.pages + ((size_t)b * a.Hkv + kvh) * a.S + e);
-            const int left = n - ((lp << shift) + off);
-            if ((unsigned)lp < (unsigned)pages_of(n, shift) && left > 0) {
+            const int left = (unsigned)lp < (unsigned)pages_of(n, shift) ? n - ((lp << shift) + off) : 0;
+            if (left > 0) {
                 const int page = scalar_load(a.t.table + (size_t)b * a.t.max_pages + lp);
                 x[i].left = left;
                 x[i].valid = min(left, 16);
@@ -333,6 +333,7 @@ __global__ __launch_bounds__(kPagedWaves * 64) __attribute__((amdgpu_waves_per_e
                 break;
             }
             before = __builtin_amdgcn_readlane(upto, 63);
+            if (w0 + 64 >= a.t.B) return;  // only where the counts change during the call
             window(w0 + 64);
         }
         const int chunks = __builtin_amdgcn_readlane(chunk_of, b - w0);
@@ -456,8 +457,9 @@ __global__ __launch_bounds__(kPagedWaves * 64) __attribute__((amdgpu_waves_per_e
         c0 = 0;
         if (++row == unit) {
             row = 0;
-            do {  // todo > 0: there is one
-                if (++b == w0 + 64) window(b);
+            do {  // todo > 0: there is one (unless the counts change during the call)
+                if (++b == a.t.B) return;
+                if (b == w0 + 64) window(b);
             } while (__builtin_amdgcn_readlane(chunk_of, b - w0) == 0);
         }
         __syncthreads();  // the parts have been read
@@ -479,6 +481,8 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedParams a)
     const int kvh = h / a.f_G, hg = h % a.f_G / 16, col = h % a.f_G % 16;
     const int2 info = reinterpret_cast<const int2*>(a.ws)[b * a.f_unit.d + kvh * a.n_hg + hg];
     if (info.x < 0) return;
+    // (what no one has written, where counts change during the call, is no place of a share)
+    if ((unsigned)(info.x >> 1) >= (unsigned)a.wgs || (unsigned)info.y >= (unsigned)(a.wgs - (info.x >> 1))) return;
     const int shares = 1 + info.y;
     const float* first = shares_of(a) + (size_t)info.x * share_floats<D>();
     const float* rest = shares_of(a) + (size_t)((info.x >> 1) + 1) * 2 * share_floats<D>();

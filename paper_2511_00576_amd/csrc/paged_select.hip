@@ -189,6 +189,14 @@ __global__ __launch_bounds__(kChooseThreads) void paged_choose_kernel(SelectPara
                           [&](int j, unsigned long long k) { sh_keys[j] = k; });
         __syncthreads();
     }
+    // the first scores, before the sequence's length is known (what lies past it is not used)
+    constexpr int EARLY = 4;
+    unsigned long long early[EARLY] = {};
+    if constexpr (!SCORE) {
+#pragma unroll
+        for (int i = 0; i < EARLY; ++i)
+            if (tid + i * kChooseThreads < a.t.max_pages) early[i] = gkeys[tid + i * kChooseThreads];
+    }
     const int held = pages_of(held_tokens(a.t, b), a.t.shift);
     int* out = a.pages + (size_t)blockIdx.x * a.S;
     if (held <= a.S) {  // all of them
@@ -205,14 +213,21 @@ __global__ __launch_bounds__(kChooseThreads) void paged_choose_kernel(SelectPara
 
     // the finite scores' range
     float low = INFINITY, high = -INFINITY;
-    for (int i = tid; i < n; i += kChooseThreads) {
-        const unsigned long long k = SCORE ? sh_keys[i] : gkeys[i];
+    auto count = [&](int i, unsigned long long k) {
         if (!SCORE && in_lds) sh_keys[i] = k;
         const float x = score_of(k);
         if (fabsf(x) < INFINITY) {
             low = fminf(low, x);
             high = fmaxf(high, x);
         }
+    };
+    if constexpr (SCORE) {
+        for (int i = tid; i < n; i += kChooseThreads) count(i, sh_keys[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < EARLY; ++i)
+            if (tid + i * kChooseThreads < n) count(tid + i * kChooseThreads, early[i]);
+        for (int i = tid + EARLY * kChooseThreads; i < n; i += kChooseThreads) count(i, gkeys[i]);
     }
     low = -wave_max(-low);
     high = wave_max(high);

@@ -730,6 +730,8 @@ class PageTable:
     are already, as they stand; else every page is free."""
 
     def __init__(self, B, page, n_pages, max_tokens, device="cuda", storage=None):
+        if page not in (16, 32, 64, 128, 256):
+            raise ValueError("a page holds 16, 32, 64, 128 or 256 tokens")
         rows = -(-max_tokens // page)
         if storage is None:
             self.n_tok = torch.zeros(B, dtype=torch.int32, device=device)
@@ -810,8 +812,9 @@ def paged_append(cache: PagedCache, k, v, slots):
         raise ValueError("slots must be [B, T]")
     B, T = slots.shape
     row = (B, s.H_kv, s.d) if k.dim() == 3 and T == 1 else (B, s.H_kv, T, s.d)
-    _call(dev, "eva_paged_append", cache.ref, _expect(k, "k", row, dt, dev), _expect(v, "v", row, dt, dev),
-          _expect(slots, "slots", (B, T), torch.int32, dev), B, T)
+    args = (_expect(k, "k", row, dt, dev), _expect(v, "v", row, dt, dev), _expect(slots, "slots", (B, T), torch.int32, dev))
+    if B > 0 and T > 0:
+        _call(dev, "eva_paged_append", cache.ref, *args, B, T)
 
 
 def paged_select(cache: PagedCache, q, n_pages: int, first: int = 1, last: int = 1):

@@ -405,6 +405,39 @@ def test_choice(B, H, Hkv, d, P, lens, S, first, last, dtype):
     check_rows(o, q, ks, vs, P, dtype, pages)
 
 
+@pytest.mark.parametrize("B,pages,Hkv", [(1, 120, 2), (2, 700, 3), (1, 4500, 1), (64, 300, 4)])
+def test_choice_by_every_route(B, pages, Hkv):
+    # scored by the choosing workgroup (few pages, or rows that fill the chip) or before it, kept in LDS or not
+    lens = [16 * pages - 3 * (i % 5) for i in range(B)]
+    lib = eva._lib.load()
+    g = torch.Generator().manual_seed(pages)
+    N = B * pages
+    t = eva.PageTable(B, 16, N, 16 * pages)
+    t.n_tok.copy_(ints(lens))
+    t.table.copy_(torch.randperm(N, generator=g).int().view(B, pages))
+    mean = torch.randn(N, Hkv, 64, generator=g)
+    empty = torch.empty(N, Hkv, 16, 64, dtype=BF16, device="cuda")
+    cache = eva.PagedCache(t, 2 * Hkv, Hkv, 64, storage=(empty, empty.view(N, Hkv, 2, 64, 8), mean.cuda()))
+    alone = lib.eva_paged_select_workspace_bytes(cache.ref, t.ref, 40) == 0
+    assert alone == (pages == 120 or B == 64)
+    q = query(B, 2 * Hkv, 64, BF16, seed=pages)
+    check_choice(cache, q, lens, 40, 2, 3)
+    # one score far above all others, and more that tie than are ranked one against the other
+    at = t.table.long()
+    mean[:] = mean[0]
+    mean[at[:, 5].cpu()] = 1e4 * q[:, ::2].float()
+    mean[at[:, 7].cpu()] = -1e4 * q[:, ::2].float()
+    mean[at[:, 20:60].cpu().flatten()] = mean[0] * 1.5
+    cache.k_mean.copy_(mean)
+    for S in (6, 30, 60, 100):
+        check_choice(cache, q, lens, S, 1, 1)
+    mean[at[:, 10:].cpu().flatten()] = NAN
+    mean[at[:, 12].cpu()] = INF
+    cache.k_mean.copy_(mean)
+    for S in (3, 40, pages - 1):
+        check_choice(cache, q, lens, S, 1, 1)
+
+
 def test_equal_scores_take_the_lower_page():
     lens = [100 * 16]
     cache, *_ = build(1, 2, 1, 64, 16, lens, F32)

@@ -94,7 +94,7 @@ def test_null_structs(lib):
 @pytest.mark.parametrize("call,kw,code", [
     (extend, dict(T=0), INVALID), (extend, dict(slots=None), INVALID), (extend, dict(start=None), INVALID),
     (extend, dict(granted=None), INVALID), (extend, dict(counts=OFF2), INVALID), (extend, dict(slots=OFF2), INVALID),
-    (extend, dict(T=2 ** 30 + 1), UNSUPPORTED), (truncate, dict(lens=None), INVALID), (truncate, dict(lens=OFF2), INVALID),
+    (extend, dict(T=2 ** 30 + 1), UNSUPPORTED), (extend, dict(t=table(B=65535), T=300000), UNSUPPORTED), (truncate, dict(lens=None), INVALID), (truncate, dict(lens=OFF2), INVALID),
     (append, dict(B=0), INVALID), (append, dict(T=0), INVALID), (append, dict(k=None), INVALID), (append, dict(v=OFF8), INVALID),
     (append, dict(slots=None), INVALID), (append, dict(slots=OFF2), INVALID), (append, dict(B=65536), UNSUPPORTED),
     (append, dict(T=2 ** 30 + 1), UNSUPPORTED), (append, dict(B=60000, T=60000), UNSUPPORTED),
@@ -155,10 +155,17 @@ def test_shapes_and_types_are_refused():
                  lambda: eva.paged_decode(c, q, pages=pages[..., :0]), lambda: eva.paged_decode(c, q, pages=pages.long()),
                  lambda: eva.paged_decode(c, q, active=n.bool()), lambda: eva.paged_decode(c, q, out=q.float()),
                  lambda: eva.paged_select(c, q, 0), lambda: eva.paged_select(c, q[:, :2], 3),
+                 lambda: eva.PageTable(2, 48, 10, 100, device="cpu"),
                  lambda: eva.PageTable(2, 16, 10, 100, device="cpu", storage=(n, n, n, n)),
                  lambda: eva.PagedCache(t, 4, 2, 64, storage=(c.k, c.k, c.k_mean))):
         with pytest.raises(ValueError):
             call()
+
+
+def test_no_tokens_are_no_call():
+    t, c = host()
+    eva.paged_append(c, torch.zeros(2, 2, 0, 64, dtype=torch.bfloat16), torch.zeros(2, 2, 0, 64, dtype=torch.bfloat16),
+                     torch.zeros(2, 0, dtype=torch.int32))
 
 
 def test_arrays_that_there_are_already():
