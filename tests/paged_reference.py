@@ -1,6 +1,22 @@
 """Plain models of the paged cache, on the CPU: the table as lists, pools built row
 by row, and the pages that a kv head's queries choose, by 64-bit scores."""
+import math
+
 import torch
+
+from rows_reference import row
+
+
+def attend(q, k, v, dtype):
+    """Rows q [heads, d] over keys and values [n, d]: (o, bound).  fp32: the bound that
+    rows_reference.py derives.  bf16: the output is rounded, half a step, 2^-8 of it; a
+    weight is cut off after 8 bits, which leaves less than 2^-7 of it, and what is left is
+    rounded in its turn, 2^-8 of that: 2^-15 of sum_j p_j |v_j|."""
+    o, bound = row(q, k, v, torch.zeros(len(k), dtype=torch.float64), torch.float32)
+    if dtype == torch.bfloat16:
+        p = torch.softmax(q.double() @ k.T / math.sqrt(q.shape[-1]), -1)
+        bound = bound + 2.0 ** -8 * o.abs() + 2.0 ** -15 * (p @ v.abs())
+    return o, bound
 
 
 class Table:
