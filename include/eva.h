@@ -788,7 +788,7 @@ int eva_paged_append(const eva_pcache* cache, const void* k_new, const void* v_n
  * ws: optional device scratch of eva_paged_decode_workspace_bytes() bytes, which
  * every call that overlaps another needs for its own: the chunks of 32 tokens of all
  * rows are shared evenly by the workgroups, and rows that several of them had are
- * joined by a second launch; with less, a workgroup takes each row (and 16 heads).
+ * joined by a second launch; with less, a workgroup takes each row.
  * The same call gives the same bits; the order of a row's sum depends on all lengths.
  * Errors: INVALID (malformed or different table and cache, null or misaligned
  * pointers, S), UNSUPPORTED (d, dtype, sizes).

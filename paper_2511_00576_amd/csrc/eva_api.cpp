@@ -1303,7 +1303,8 @@ struct PagedRoute {
     int n_hg;
 };
 int paged_route(PagedRoute& r, const eva_pcache* c, const eva_page_table* t, int S) {
-    r.n_hg = (c->H / c->H_kv + 15) / 16;
+    const int G = c->H / c->H_kv, per = 16 * eva::paged_tiles(G);
+    r.n_hg = (int)(((long long)G + per - 1) / per);
     r.rows = (long long)t->B * c->H_kv * r.n_hg;
     const long long pages = S > 0 && S < t->max_pages ? S : t->max_pages;
     const int tokens = 16 * eva::paged_blocks(c->d, c->dtype == EVA_F32 ? 4 : 2);
@@ -1386,7 +1387,7 @@ int eva_paged_select(const eva_pcache* cache, const eva_page_table* table, const
 size_t eva_paged_decode_workspace_bytes(const eva_pcache* cache, const eva_page_table* table, int S) {
     PagedRoute r;
     if (check_paged(cache, table) != EVA_OK || S < 0 || paged_route(r, cache, table, S) != EVA_OK || r.wgs == 0) return 0;
-    return eva::paged_ws_bytes(r.rows, r.wgs, cache->d);
+    return eva::paged_ws_bytes(r.rows, r.wgs, cache->d, cache->H / cache->H_kv);
 }
 
 int eva_paged_decode(const eva_pcache* cache, const eva_page_table* table, const void* q, void* o, const int* pages, int S,
@@ -1418,8 +1419,9 @@ int eva_paged_decode(const eva_pcache* cache, const eva_page_table* table, const
     p.f_H = eva::FastDiv(cache->H);
     p.f_G = eva::FastDiv(p.G);
     p.scale_log2 = (float)(1.4426950408889634 / sqrt((double)cache->d));
-    if (r.wgs > 0 && ws && aligned16(ws) && ws_bytes >= eva::paged_ws_bytes(r.rows, r.wgs, cache->d))
+    if (r.wgs > 0 && ws && aligned16(ws) && ws_bytes >= eva::paged_ws_bytes(r.rows, r.wgs, cache->d, p.G))
         p.ws = static_cast<float*>(ws);
+    p.alone = r.wgs == 0 && r.rows >= eva::kPagedMany;
     hipStream_t s = static_cast<hipStream_t>(stream);
     return hip_status(dispatch(cache->d, cache->dtype, [&](auto dd, auto t) {
         return eva::launch_paged_decode<decltype(dd)::value, decltype(t)>(p, s);

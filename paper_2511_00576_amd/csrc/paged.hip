@@ -1,7 +1,8 @@
 // Decode over a paged cache: one query per sequence attends all its tokens, or
 // those of a list of pages.
 //
-// A row is (sequence, kv head, group of up to 16 query heads); its keys go by
+// A row is (sequence, kv head, group of up to 16 query heads, or 32 where a kv head has more
+// than 16: NC = 2 tiles of columns share the operands); its keys go by
 // chunks of one or two blocks of 16 tokens, each of which lies in one page.  Per
 // chunk a wave computes S^T = K Q^T and O^T += V^T P^T on the matrix cores with
 // the operands read straight from memory, 16 bytes a lane, the softmax's maximum
@@ -10,8 +11,9 @@
 // The batch's rows may differ in length by any factor, and their lengths are on
 // the device.  So the launch has a fixed number of workgroups, and they share the
 // chunks of all rows, one row after the other, in equal contiguous parts: a
-// workgroup finds its part from the sequences' token counts (a scan, a microsecond),
-// and rows that lie in more than one part are joined by a second launch.
+// workgroup finds its part from the sequences' token counts (a scan, half a microsecond),
+// and rows that lie in more than one part are joined by a second launch.  Where rows are
+// short and many, every wave takes rows of its own, whole ones: no barrier, no joining.
 #include "paged.hpp"
 
 namespace eva {
@@ -289,21 +291,22 @@ __device__ __forceinline__ floatx4 finish(float m, float l, const floatx4& o) {
 
 // Workspace: an int2 for each row (x: -1, or 2 w + s for a row whose first part is share
 // s of workgroup w; y: how many workgroups after w hold the rest), then [wgs][2] shares
-// of 16 columns: maximum, sum, two floats unused, [D] weighted values.  Share 0 is that of a part's first row,
+// of 16 NC columns: maximum, sum, two floats unused, [D] weighted values.  Share 0 is that of a part's first row,
 // share 1 that of its last one.
-template <int D>
-__host__ __device__ constexpr int share_floats() { return 16 * share_col(D); }
+template <int D, int NC>
+__host__ __device__ constexpr int share_floats() { return 16 * NC * share_col(D); }
 __device__ __forceinline__ float* shares_of(const PagedParams& a) { return a.ws + (a.rows + 1) / 2 * 4; }
 
-template <int D, typename T>
-__global__ __launch_bounds__(kPagedWaves * 64) __attribute__((amdgpu_waves_per_eu(3, 8))) void paged_decode_kernel(PagedParams a) {
+template <int D, typename T, int NC>
+__global__ __launch_bounds__(kPagedWaves * 64) __attribute__((amdgpu_waves_per_eu(NC == 1 ? 3 : 2, 8)))
+void paged_decode_kernel(PagedParams a) {
     constexpr int NW = kPagedWaves;
     constexpr int COL = D + 4;  // 16 columns on distinct banks
     typedef typename QueryFragment<T>::type Frag;
     constexpr int NQ = D / QueryFragment<T>::kFeatures;
     constexpr int NB = Chunk<D, T>::kBlocks;
-    __shared__ float red_m[NW][16], red_l[NW][16];
-    __shared__ __attribute__((aligned(16))) float red_o[NW][16][COL];
+    __shared__ float red_m[NW][16 * NC], red_l[NW][16 * NC];
+    __shared__ __attribute__((aligned(16))) float red_o[NW][16 * NC][COL];
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -312,9 +315,11 @@ __global__ __launch_bounds__(kPagedWaves * 64) __attribute__((amdgpu_waves_per_e
     const T* kp = static_cast<const T*>(a.k);
     const T* vp = static_cast<const T*>(a.vt);
 
-    // this workgroup's chunks: `todo` from chunk c0 of row `row` of sequence b on.  The
-    // lanes hold 64 sequences' counts at a time, w0 the first of them.
-    int b, row, c0, todo, part = 0, w0, tokens, chunk_of;
+    // This workgroup's part: `todo` chunks from chunk c0 of row `row` of sequence b on; or,
+    // where rows are short and many (`alone`), this wave's: `todo` rows.  The lanes hold 64
+    // sequences' counts at a time, w0 the first of them.
+    int b, row, c0 = 0, todo, part = 0, w0, tokens, chunk_of;
+    bool alone;
     auto window = [&](int from) {
         w0 = from;
         const int i = min(from + lane, a.t.B - 1);
@@ -323,65 +328,79 @@ __global__ __launch_bounds__(kPagedWaves * 64) __attribute__((amdgpu_waves_per_e
     };
     if (a.ws) {
         window(0);
-        int total = chunk_of;
-        for (int i = 64; i < a.t.B; i += 64)
-            if (i + lane < a.t.B) total += row_chunks<16 * NB>(a, i + lane, held_tokens(a.t, i + lane));
-        total = __builtin_amdgcn_readlane(wave_scan(total), 63) * unit;
-        part = max((total + a.wgs - 1) / a.wgs, kPagedMinPart);
-        const int from = (int)blockIdx.x * part;
+        int chunks = chunk_of, longest = chunk_of, rows = chunk_of > 0;
+        for (int i = 64; i < a.t.B; i += 64) {
+            const int more = i + lane < a.t.B ? row_chunks<16 * NB>(a, i + lane, held_tokens(a.t, i + lane)) : 0;
+            chunks += more;
+            longest = max(longest, more);
+            rows += more > 0;
+        }
+        rows = __builtin_amdgcn_readlane(wave_scan(rows), 63) * unit;
+        alone = __builtin_amdgcn_readlane(wave_max(longest), 63) <= (rows >= kPagedMany ? kPagedShort : kPagedShortest);
+        const int total = alone ? rows : __builtin_amdgcn_readlane(wave_scan(chunks), 63) * unit;
+        const int workers = alone ? a.wgs * NW : a.wgs, me = alone ? (int)blockIdx.x * NW + wave : (int)blockIdx.x;
+        part = max((total + workers - 1) / workers, alone ? 1 : kPagedMinPart);
+        const long long from = (long long)me * part;
         if (from >= total) return;
-        todo = min(part, total - from);
-        // the sequence that holds chunk `from`
+        todo = min(part, total - (int)from);
+        // the sequence that holds chunk (or row) `from`
         int before = 0, at;
         while (true) {
-            const int upto = before + wave_scan(chunk_of * unit);
-            const unsigned long long past = __builtin_amdgcn_ballot_w64(upto > from);
+            const int mine = (alone ? chunk_of > 0 : chunk_of) * unit;
+            const int upto = before + wave_scan(mine);
+            const unsigned long long past = __builtin_amdgcn_ballot_w64(upto > (int)from);
             if (past) {
                 const int l = __builtin_ctzll(past);
                 b = w0 + l;
-                at = from - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(chunk_of, l) * unit);
+                at = (int)from - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(mine, l));
                 break;
             }
             before = __builtin_amdgcn_readlane(upto, 63);
             if (w0 + 64 >= a.t.B) return;  // only where the counts change during the call
             window(w0 + 64);
         }
-        const int chunks = __builtin_amdgcn_readlane(chunk_of, b - w0);
-        row = at / chunks;
-        c0 = at - row * chunks;
+        const int each = alone ? 1 : __builtin_amdgcn_readlane(chunk_of, b - w0);
+        row = at / each;
+        c0 = at - row * each;
     } else {
-        b = (int)blockIdx.x / a.f_unit;
-        row = (int)blockIdx.x % a.f_unit;
-        c0 = 0;
+        alone = a.alone;
+        const int r = alone ? (int)blockIdx.x * NW + wave : (int)blockIdx.x;
+        if (r >= a.rows) return;
+        b = r / a.f_unit;
+        row = r % a.f_unit;
         window(b / 64 * 64);
-        todo = __builtin_amdgcn_readlane(chunk_of, b - w0);
-        if (todo == 0) return;
+        const int chunks = __builtin_amdgcn_readlane(chunk_of, b - w0);
+        if (chunks == 0) return;
+        todo = alone ? 1 : chunks;
     }
     b = __builtin_amdgcn_readfirstlane(b);
     row = __builtin_amdgcn_readfirstlane(row);
     c0 = __builtin_amdgcn_readfirstlane(c0);
     todo = __builtin_amdgcn_readfirstlane(todo);
+    const int step = alone ? 1 : NW;
 
     for (bool first = true;; first = false) {
         const int n = __builtin_amdgcn_readlane(tokens, b - w0);
         const int n_pages = row_pages(a, n);
         const int chunks = __builtin_amdgcn_readlane(chunk_of, b - w0);
-        const int c1 = min(chunks, c0 + todo);
+        const int c1 = alone ? chunks : min(chunks, c0 + todo);
         const int kvh = row / a.f_hg, hg = row % a.f_hg;
-        const int h0 = kvh * a.G + hg * 16;
-        const int ncols = min(16, a.G - hg * 16);
+        const int h0 = kvh * a.G + hg * 16 * NC;
+        const int ncols = min(16 * NC, a.G - hg * 16 * NC);
         // columns past ncols repeat the last head; their outputs are not stored
-        Frag q[NQ];
-        Chunk<D, T>::query(q, static_cast<const T*>(a.q) + ((size_t)b * a.H + h0 + min(c16, ncols - 1)) * D, g);
-
-        RowState<D> st;
-        st.clear();
+        Frag q[NC][NQ];
+        RowState<D> st[NC];
+#pragma unroll
+        for (int t = 0; t < NC; ++t) {
+            Chunk<D, T>::query(q[t], static_cast<const T*>(a.q) + ((size_t)b * a.H + h0 + min(16 * t + c16, ncols - 1)) * D, g);
+            st[t].clear();
+        }
         bool any = false;
         // a chunk's keys are requested while the one before is weighed, its values once
         // that one's have been used: the wave always has half a chunk in flight
         Chunk<D, T> rows;
         Block x[NB];
-        int ch = c0 + wave;
+        int ch = alone ? 0 : c0 + wave;
         if (ch < c1) {
             locate<D, NB>(x, a, b, kvh, n, n_pages, ch);
             rows.load_keys(kp, x, g, c16);
@@ -396,11 +415,12 @@ __global__ __launch_bounds__(kPagedWaves * 64) __attribute__((amdgpu_waves_per_e
                 lost |= (x[i].lost ? 0xffffu : 0u) << (16 * i);
             }
             any = any || valid != 0;
-            ch += NW;
+            ch += step;
             const bool more = ch < c1;
             if (more) locate<D, NB>(x, a, b, kvh, n, n_pages, ch);
-            floatx4 s[NB];
-            rows.scores(q, s);
+            floatx4 s[NC][NB];
+#pragma unroll
+            for (int t = 0; t < NC; ++t) rows.scores(q[t], s[t]);
             __builtin_amdgcn_sched_barrier(0);
             if (more) rows.load_keys(kp, x, g, c16);
             if (valid != 0xffffffffu >> (32 - 16 * NB) || lost) {
@@ -408,61 +428,83 @@ __global__ __launch_bounds__(kPagedWaves * 64) __attribute__((amdgpu_waves_per_e
                 for (int kb = 0; kb < NB; ++kb) {
                     const int in = Chunk<D, T>::mask_of(valid, g, kb), no = Chunk<D, T>::mask_of(lost, g, kb);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) s[kb][i] = in >> i & 1 ? no >> i & 1 ? NAN : s[kb][i] : -INFINITY;
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int t = 0; t < NC; ++t)
+                            s[t][kb][i] = in >> i & 1 ? no >> i & 1 ? NAN : s[t][kb][i] : -INFINITY;
                 }
                 rows.keep_values(valid, g);
             }
-            st.weigh(s, a.scale_log2);
-            rows.add(s, st.acc);
+#pragma unroll
+            for (int t = 0; t < NC; ++t) {
+                st[t].weigh(s[t], a.scale_log2);
+                rows.add(s[t], st[t].acc);
+            }
             __builtin_amdgcn_sched_barrier(0);
             if (more) rows.load_values(vp, x, g, c16);
         }
 
         // ---- the waves' parts of the row ----
-        float l = xgroup_sum(st.l);
-        if (any && st.m == -INFINITY && l == 0.f) l = -1.f;  // see finish()
-        if (g == 0) {
-            red_m[wave][c16] = st.m;
-            red_l[wave][c16] = l;
-        }
-        if (c16 < ncols) {
+        bool whole = true;
 #pragma unroll
-            for (int i = 0; i < D / 16; ++i) *reinterpret_cast<floatx4*>(&red_o[wave][c16][16 * i + 4 * g]) = st.acc[i];
-        }
-        __syncthreads();
-        const bool whole = c0 == 0 && c1 == chunks;
-        const int share = first ? 0 : 1;
-        float* part_ws = a.ws ? shares_of(a) + ((size_t)blockIdx.x * 2 + share) * share_floats<D>() : nullptr;
-        for (int t = tid; t < ncols * (D / 4); t += NW * 64) {
-            const int col = t / (D / 4), f = t % (D / 4) * 4;
-            float m = -INFINITY, sum = 0.f;
-            floatx4 o = {0.f, 0.f, 0.f, 0.f};
+        for (int t = 0; t < NC; ++t) {
+            const int col = 16 * t + c16;
+            float l = xgroup_sum(st[t].l);
+            if (any && st[t].m == -INFINITY && l == 0.f) l = -1.f;  // see finish()
+            if (alone) {
+                if (col < ncols) {
+                    T* o = static_cast<T*>(a.o) + ((size_t)b * a.H + h0 + col) * D + 4 * g;
 #pragma unroll
-            for (int w = 0; w < NW; ++w) m = fmaxf(m, red_m[w][col]);
-#pragma unroll
-            for (int w = 0; w < NW; ++w) {
-                // without a maximum there is no weight; sums of NaN stay, and where there is none at
-                // all the waves' reasons are summed as they are
-                const float mw = red_m[w][col];
-                const float wt = m == -INFINITY ? 1.f : mw == -INFINITY ? 0.f : fast_exp2(mw - m);
-                sum += wt * red_l[w][col];
-                o += wt * *reinterpret_cast<const floatx4*>(&red_o[w][col][f]);
+                    for (int i = 0; i < D / 16; ++i) store4(o + 16 * i, finish(st[t].m, l, st[t].acc[i]));
+                }
+                continue;
             }
-            if (whole) {
-                store4(static_cast<T*>(a.o) + ((size_t)b * a.H + h0 + col) * D + f, finish(m, sum, o));
-            } else {
-                float* to = part_ws + col * share_col(D);
-                if (f == 0) *reinterpret_cast<floatx2*>(to) = floatx2{m, sum};
-                *reinterpret_cast<floatx4*>(to + 4 + f) = o;
+            if (g == 0) {
+                red_m[wave][col] = st[t].m;
+                red_l[wave][col] = l;
+            }
+            if (col < ncols) {
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i)
+                    *reinterpret_cast<floatx4*>(&red_o[wave][col][16 * i + 4 * g]) = st[t].acc[i];
+            }
+        }
+        const int share = first ? 0 : 1;
+        if (!alone) {
+            __syncthreads();
+            whole = c0 == 0 && c1 == chunks;
+            float* part_ws = a.ws ? shares_of(a) + ((size_t)blockIdx.x * 2 + share) * share_floats<D, NC>() : nullptr;
+            for (int t = tid; t < ncols * (D / 4); t += NW * 64) {
+                const int col = t / (D / 4), f = t % (D / 4) * 4;
+                float m = -INFINITY, sum = 0.f;
+                floatx4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int w = 0; w < NW; ++w) m = fmaxf(m, red_m[w][col]);
+#pragma unroll
+                for (int w = 0; w < NW; ++w) {
+                    // without a maximum there is no weight; sums of NaN stay, and where there is none at
+                    // all the waves' reasons are summed as they are
+                    const float mw = red_m[w][col];
+                    const float wt = m == -INFINITY ? 1.f : mw == -INFINITY ? 0.f : fast_exp2(mw - m);
+                    sum += wt * red_l[w][col];
+                    o += wt * *reinterpret_cast<const floatx4*>(&red_o[w][col][f]);
+                }
+                if (whole) {
+                    store4(static_cast<T*>(a.o) + ((size_t)b * a.H + h0 + col) * D + f, finish(m, sum, o));
+                } else {
+                    float* to = part_ws + col * share_col(D);
+                    if (f == 0) *reinterpret_cast<floatx2*>(to) = floatx2{m, sum};
+                    *reinterpret_cast<floatx4*>(to + 4 + f) = o;
+                }
             }
         }
         if (!a.ws) return;
-        if (c0 == 0 && tid == 0) {
+        if (c0 == 0 && (alone ? lane : tid) == 0) {
             int2 info = {-1, 0};
             if (!whole) info = int2{2 * (int)blockIdx.x + share, (chunks - c1 + part - 1) / part};
             reinterpret_cast<int2*>(a.ws)[b * unit + row] = info;
         }
-        todo -= c1 - c0;
+        todo -= alone ? 1 : c1 - c0;
         if (todo == 0) return;
         c0 = 0;
         if (++row == unit) {
@@ -472,15 +514,40 @@ __global__ __launch_bounds__(kPagedWaves * 64) __attribute__((amdgpu_waves_per_e
                 if (b == w0 + 64) window(b);
             } while (__builtin_amdgcn_readlane(chunk_of, b - w0) == 0);
         }
-        __syncthreads();  // the parts have been read
+        if (!alone) __syncthreads();  // the parts have been read
     }
 }
 
 // Joins the shares of rows that more than one workgroup held: a workgroup per query
-// head (one per row would read all its columns through one CU: JOIN_FIGURES), threads
-// over (share, four features), then over LDS.
+// head, whose threads, four features each, divide the shares and meet in LDS (one sequence
+// of 8000 tokens, 63 shares a row: 13.8 us the whole decode, 15.3 with a workgroup per row that
+// reads all its columns through one CU).
 constexpr int kJoinThreads = 256;
-template <int D, typename T>
+template <int D>
+struct Joined {
+    float m = -INFINITY, l = 0.f;
+    floatx4 o = {0.f, 0.f, 0.f, 0.f};
+    template <int N>
+    __device__ __forceinline__ void add(const float (&mx)[N], const float (&lx)[N], const floatx4 (&ox)[N]) {
+        float top = m;
+#pragma unroll
+        for (int i = 0; i < N; ++i) top = fmaxf(top, mx[i]);
+        // without a maximum there is no weight; sums of NaN stay, and where there is none at
+        // all the reasons (finish()) are summed as they are
+        const float keep = top == -INFINITY ? 1.f : m == -INFINITY ? 0.f : fast_exp2(m - top);
+        l *= keep;
+        o *= keep;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float wt = top == -INFINITY ? 1.f : mx[i] == -INFINITY ? 0.f : fast_exp2(mx[i] - top);
+            l += wt * lx[i];
+            o += wt * ox[i];
+        }
+        m = top;
+    }
+};
+
+template <int D, typename T, int NC>
 __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedParams a) {
     constexpr int ITEMS = D / 4, GROUPS = kJoinThreads / ITEMS;
     constexpr int NB = 4;  // shares whose loads are in flight together
@@ -488,79 +555,69 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedParams a)
     __shared__ __attribute__((aligned(16))) floatx4 red_o[GROUPS][ITEMS];
     const int b = (int)blockIdx.x / a.f_H, h = (int)blockIdx.x % a.f_H;
     if (a.active && a.active[b] == 0) return;  // no one has written its entry
-    const int kvh = h / a.f_G, hg = h % a.f_G / 16, col = h % a.f_G % 16;
+    const int kvh = h / a.f_G, hg = h % a.f_G / (16 * NC), col = h % a.f_G % (16 * NC);
     const int2 info = reinterpret_cast<const int2*>(a.ws)[b * a.f_unit.d + kvh * a.n_hg + hg];
     if (info.x < 0) return;
     // (what no one has written, where counts change during the call, is no place of a share)
     if ((unsigned)(info.x >> 1) >= (unsigned)a.wgs || (unsigned)info.y >= (unsigned)(a.wgs - (info.x >> 1))) return;
     const int shares = 1 + info.y;
-    const float* first = shares_of(a) + (size_t)info.x * share_floats<D>();
-    const float* rest = shares_of(a) + (size_t)((info.x >> 1) + 1) * 2 * share_floats<D>();
+    const float* first = shares_of(a) + (size_t)info.x * share_floats<D, NC>();
+    const float* rest = shares_of(a) + (size_t)((info.x >> 1) + 1) * 2 * share_floats<D, NC>();
     const int grp = threadIdx.x / ITEMS, f = threadIdx.x % ITEMS * 4;
-    float M = -INFINITY, L = 0.f;
-    floatx4 O = {0.f, 0.f, 0.f, 0.f};
+    Joined<D> j;
     for (int s0 = grp; s0 < shares; s0 += GROUPS * NB) {
         float m[NB], l[NB];
         floatx4 o[NB];
 #pragma unroll
         for (int i = 0; i < NB; ++i) {
             const int s = min(s0 + i * GROUPS, shares - 1);
-            const float* w = (s == 0 ? first : rest + (size_t)(s - 1) * 2 * share_floats<D>()) + col * share_col(D);
+            const float* w = (s == 0 ? first : rest + (size_t)(s - 1) * 2 * share_floats<D, NC>()) + col * share_col(D);
             const floatx2 ml = *reinterpret_cast<const floatx2*>(w);
             m[i] = ml[0];
             l[i] = ml[1];
             o[i] = *reinterpret_cast<const floatx4*>(w + 4 + f);
         }
-        float top = M;
 #pragma unroll
-        for (int i = 0; i < NB; ++i) {
+        for (int i = 0; i < NB; ++i)
             if (s0 + i * GROUPS >= shares) {  // past the last
                 m[i] = -INFINITY;
                 l[i] = 0.f;
                 o[i] = floatx4{0.f, 0.f, 0.f, 0.f};
             }
-            top = fmaxf(top, m[i]);
-        }
-        const float keep = top == -INFINITY ? 1.f : M == -INFINITY ? 0.f : fast_exp2(M - top);
-        L *= keep;
-        O *= keep;
-#pragma unroll
-        for (int i = 0; i < NB; ++i) {
-            const float wt = top == -INFINITY ? 1.f : m[i] == -INFINITY ? 0.f : fast_exp2(m[i] - top);
-            L += wt * l[i];
-            O += wt * o[i];
-        }
-        M = top;
+        j.add(m, l, o);
     }
     if (f == 0) {
-        red_m[grp] = M;
-        red_l[grp] = L;
+        red_m[grp] = j.m;
+        red_l[grp] = j.l;
     }
-    red_o[grp][f / 4] = O;
+    red_o[grp][f / 4] = j.o;
     __syncthreads();
     if (grp != 0) return;
-    float top = M;
-#pragma unroll
-    for (int i = 1; i < GROUPS; ++i) top = fmaxf(top, red_m[i]);
-    float sum = 0.f;
-    floatx4 out = {0.f, 0.f, 0.f, 0.f};
+    float m[GROUPS], l[GROUPS];
+    floatx4 o[GROUPS];
 #pragma unroll
     for (int i = 0; i < GROUPS; ++i) {
-        const float m = red_m[i];
-        const float wt = top == -INFINITY ? 1.f : m == -INFINITY ? 0.f : fast_exp2(m - top);
-        sum += wt * red_l[i];
-        out += wt * red_o[i][f / 4];
+        m[i] = red_m[i];
+        l[i] = red_l[i];
+        o[i] = red_o[i][f / 4];
     }
-    store4(static_cast<T*>(a.o) + (size_t)blockIdx.x * D + f, finish(top, sum, out));
+    Joined<D> all;
+    all.add(m, l, o);
+    store4(static_cast<T*>(a.o) + (size_t)blockIdx.x * D + f, finish(all.m, all.l, all.o));
 }
 
 }  // namespace
 
+template <int D, typename T, int NC>
+static hipError_t launch_columns(const PagedParams& p, hipStream_t stream) {
+    const int wgs = p.ws ? p.wgs : p.alone ? (p.rows + kPagedWaves - 1) / kPagedWaves : p.rows;
+    paged_decode_kernel<D, T, NC><<<wgs, kPagedWaves * 64, 0, stream>>>(p);
+    if (p.ws) paged_join_kernel<D, T, NC><<<p.t.B * p.H, kJoinThreads, 0, stream>>>(p);
+    return hipGetLastError();
+}
 template <int D, typename T>
 hipError_t launch_paged_decode(const PagedParams& p, hipStream_t stream) {
-    paged_decode_kernel<D, T><<<p.ws ? p.wgs : p.rows, kPagedWaves * 64, 0, stream>>>(p);
-    if (p.ws) paged_join_kernel<D, T><<<p.t.B * p.H, kJoinThreads, 0, stream>>>(p);
-    return hipGetLastError();
+    return paged_tiles(p.G) == 1 ? launch_columns<D, T, 1>(p, stream) : launch_columns<D, T, 2>(p, stream);
 }
 template hipError_t launch_paged_decode<64, bf16>(const PagedParams&, hipStream_t);
 template hipError_t launch_paged_decode<128, bf16>(const PagedParams&, hipStream_t);

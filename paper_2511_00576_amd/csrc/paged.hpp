@@ -51,6 +51,17 @@ __device__ __forceinline__ I wave_scan(I x) {
     return x;
 }
 
+// Largest of the wave's values, none of them negative, in lane 63.
+__device__ __forceinline__ int wave_max(int x) {
+    x = max(x, dpp<0x111>(x));
+    x = max(x, dpp<0x112>(x));
+    x = max(x, dpp<0x114>(x));
+    x = max(x, dpp<0x118>(x));
+    x = max(x, dpp<0x142, 0xa>(x));
+    x = max(x, dpp<0x143, 0xc>(x));
+    return x;
+}
+
 // Inclusive sum over the workgroup's threads, and the whole sum; sums has room for
 // every wave's.
 template <typename I>
@@ -97,9 +108,10 @@ struct PagedParams {
     void* o;
     float* ws;          // partials of split rows, nullptr: a workgroup per row
     int S, H, Hkv, G;
-    int n_hg;           // groups of 16 query heads of a kv head
+    int n_hg;           // groups of 16 paged_tiles(G) query heads of a kv head
     int rows;           // B Hkv n_hg
     int wgs;            // workgroups that share all rows' chunks (with ws)
+    int alone;          // without ws: a wave per row, not a workgroup
     FastDiv f_unit, f_hg;  // divisors of Hkv n_hg and of n_hg
     FastDiv f_H, f_G;      // of H and of G
     float scale_log2;
@@ -109,13 +121,27 @@ struct PagedParams {
 constexpr int paged_blocks(int d, int bytes) { return bytes == 4 && d == 128 ? 1 : 2; }
 // The fewest chunks a workgroup takes: one for each of its four waves.
 constexpr int kPagedMinPart = 4;
+// Rows of up to kPagedShortest chunks go to one wave each, and of up to kPagedShort where
+// there are kPagedMany and more.  us in a replayed graph, a wave / a workgroup (which takes
+// kPagedMinPart chunks and more, however many rows that is), bf16 d = 128, chunks of 32 tokens:
+//     rows   1 chunk     2           4           8
+//      256   6.9 / 12.4  8.0 / 9.2   10.1 / 7.6  18.7 / 11.8
+//      512   7.1 / 12.6  8.1 / 9.4   12.8 / 9.9  21 / 15
+//     1024   8.1 / 13.7  10.5 / 12.2 15.6 / 15.7 26.2 / 26.6
+//     4096   24 / 33     33 / 40     53 / 58     92 / 99
+// Where no row can have more than kPagedMinPart chunks there is a workgroup per row, and a wave
+// per row from kPagedMany on (1 chunk: 512 rows 4.8 / 4.8, 1024 4.9 / 7.2, 4096 14.7 / 22.7).
+constexpr int kPagedShortest = 2, kPagedShort = 8, kPagedMany = 1024;
 // Workgroups that share a decode's chunks: as many as the CUs hold at once.
 constexpr int kPagedWgs = 512;
+// Tiles of 16 query heads that a workgroup has at once: with two, what a kv head's more than
+// 16 heads read is read once for 32 of them (PAGED_NC_FIGURES).
+constexpr int paged_tiles(int G) { return G > 16 ? 2 : 1; }
 // Floats of a column of a share (paged.hip).
 __host__ __device__ constexpr int share_col(int d) { return d + 4; }
 // Bytes of the workspace: a pair of ints per row, then two shares per workgroup.
-inline size_t paged_ws_bytes(long long rows, long long wgs, int d) {
-    return ((size_t)(rows + 1) / 2 * 4 + (size_t)wgs * 2 * 16 * share_col(d)) * sizeof(float);
+inline size_t paged_ws_bytes(long long rows, long long wgs, int d, int G) {
+    return ((size_t)(rows + 1) / 2 * 4 + (size_t)wgs * 2 * 16 * paged_tiles(G) * share_col(d)) * sizeof(float);
 }
 template <int D, typename T>
 hipError_t launch_paged_decode(const PagedParams& p, hipStream_t stream);

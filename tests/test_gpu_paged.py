@@ -245,6 +245,31 @@ def test_decode_shares_long_rows(P, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("B,H,Hkv,longest,most", [
+    (6, 6, 3, 32, 5000),       # rows so short that a wave takes each
+    (150, 16, 8, 120, 5000),   # many rows, of up to eight chunks
+    (150, 16, 8, 60, 64),      # many, in a table with room for no more
+    (70, 40, 2, 100, 5000),    # 20 heads a kv head
+    (300, 6, 4, 31, 31),       # 1200 rows of one chunk
+])
+def test_short_rows(B, H, Hkv, longest, most, dtype):
+    if H % Hkv:
+        H = Hkv
+    lens = [(i * 53) % (longest + 1) for i in range(B)]
+    cache, ks, vs = build(B, H, Hkv, 64, 16, lens, dtype, seed=longest, most=most)
+    q = query(B, H, 64, dtype)
+    active = [int(i % 9 != 4) for i in range(B)]
+    for ws in (True, False):
+        out = torch.full((B, H, 64), 3.0, dtype=dtype, device="cuda")
+        o = eva.paged_decode(cache, q.cuda(), active=ints(active), out=out, use_workspace=ws)
+        check_rows(o, q, ks, vs, 16, dtype, skip=[b for b in range(B) if not active[b]])
+        assert (o[ints(active) == 0] == 3).all()
+        lists = [[[(b + h) % 3, 7, -1, 0] for h in range(Hkv)] for b in range(B)]
+        o = eva.paged_decode(cache, q.cuda(), pages=ints(lists), use_workspace=ws)
+        check_rows(o, q, ks, vs, 16, dtype, lists)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 def test_inactive_and_empty_rows(dtype):
     lens = [40, 500, 0, 33, 0]
     cache, ks, vs = build(5, 4, 2, 64, 16, lens, dtype)
