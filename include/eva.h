@@ -693,8 +693,8 @@ size_t eva_qtree_workspace_bytes(const eva_qcache* cache, int T);
  *   table       [B][max_pages]  pages in their order; -1 where there is none (start: -1)
  *   free_pages  [n_pages]       a stack of the pages that nobody has: the first
  *   n_free      [1]             n_free of them (start: every page, n_pages)
- * P is 16, 32, 64, 128 or 256.  Limits: n_pages P and max_pages P at most 2^30, B max_pages
- * below 2^31, B and B H_kv at most 65535 (UNSUPPORTED).  Counts outside what a
+ * P is 16, 32, 64, 128 or 256.  Limits: n_pages P, max_pages P and B max_pages at most
+ * 2^30, B and B H_kv at most 65535, B H below 2^24 (UNSUPPORTED).  Counts outside what a
  * sequence has room for are read as the nearest one inside.  Two sequences may name the same
  * pages (a common prompt) where the caller writes the table: eva_paged_decode and
  * eva_paged_select read them, but eva_page_truncate gives back what each of them names.
@@ -803,7 +803,8 @@ size_t eva_paged_decode_workspace_bytes(const eva_pcache* cache, const eva_page_
  * else its `first` first ones, its `last` last ones (the page that is being filled among them)
  * and of the others those with the highest
  *     score_j = max over the kv head's query heads of q . k_mean[page j]
- * (64-bit sums; of equal scores the lower page's, a NaN above all).  q [B][H][d].
+ * (64-bit sums; of equal scores the lower page's; a NaN, and a page that the pool does not
+ * have, above all).  q [B][H][d].
  * 0 <= first, 1 <= last, first + last <= S.  The scores need a mean of every complete page.
  * ws: device scratch of eva_paged_select_workspace_bytes() bytes (0: none needed);
  * every byte the call reads it writes first.

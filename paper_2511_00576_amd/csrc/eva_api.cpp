@@ -1263,9 +1263,9 @@ int check_table(const eva_page_table* t) {
     const void* arrays[] = {t->n_tok, t->table, t->free_pages, t->n_free};
     for (const void* p : arrays)
         if (!p || !aligned4(p)) return EVA_ERR_INVALID;
-    // slots and positions stay below 2^30, entries of the table and workgroups in 32 bits
+    // slots, positions and entries of the table stay below 2^30
     if (t->n_pages > kMaxLen / t->P || t->max_pages > kMaxLen / t->P || t->B > 65535 ||
-        (long long)t->B * t->max_pages > 0x7fffffffLL)
+        (long long)t->B * t->max_pages > kMaxLen)
         return EVA_ERR_UNSUPPORTED;
     return EVA_OK;
 }

@@ -6,7 +6,10 @@
 // chunks of one or two blocks of 16 tokens, each of which lies in one page.  Per
 // chunk a wave computes S^T = K Q^T and O^T += V^T P^T on the matrix cores with
 // the operands read straight from memory, 16 bytes a lane, the softmax's maximum
-// and sum running: every key and value is read once for the heads that share it.
+// and sum running: every key and value is read once for the heads that share it, past
+// the caches (with loads that keep them, 64 sequences at 8k take 249 us instead of 218,
+// 6.6 TB/s).  Bound by memory; calls of few tokens by the chain counts -> table -> keys ->
+// softmax -> join, 14 us for one sequence of 8000 (32 MB).
 //
 // The batch's rows may differ in length by any factor, and their lengths are on
 // the device.  So the launch has a fixed number of workgroups, and they share the

@@ -135,7 +135,8 @@ constexpr int kPagedShortest = 2, kPagedShort = 8, kPagedMany = 1024;
 // Workgroups that share a decode's chunks: as many as the CUs hold at once.
 constexpr int kPagedWgs = 512;
 // Tiles of 16 query heads that a workgroup has at once: with two, what a kv head's more than
-// 16 heads read is read once for 32 of them (PAGED_NC_FIGURES).
+// 16 heads read is read once for 32 of them (20 heads, 256 sequences of up to 4096 tokens, 2 kv
+// heads, 720 MB: 139 us against 236).
 constexpr int paged_tiles(int G) { return G > 16 ? 2 : 1; }
 // Floats of a column of a share (paged.hip).
 __host__ __device__ constexpr int share_col(int d) { return d + 4; }

