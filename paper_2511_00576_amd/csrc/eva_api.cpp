@@ -1310,10 +1310,10 @@ int paged_route(PagedRoute& r, const eva_pcache* c, const eva_page_table* t, int
     const int tokens = 16 * eva::paged_blocks(c->d, c->dtype == EVA_F32 ? 4 : 2);
     const long long chunks = (pages * t->P + tokens - 1) / tokens;
     // (threads of a launch stay below 2^32)
-    if (r.rows * chunks > 0x7fffffffLL || (long long)t->B * c->H > 0xffffff) return EVA_ERR_UNSUPPORTED;
+    if (r.rows * chunks > kMaxLen || (long long)t->B * c->H > 0xffffff) return EVA_ERR_UNSUPPORTED;
     r.wgs = 0;
     if (chunks > eva::kPagedMinPart) {
-        const long long parts = (r.rows * chunks + eva::kPagedMinPart - 1) / eva::kPagedMinPart;
+        const long long parts = r.rows * ((chunks + eva::kPagedMinPart - 1) / eva::kPagedMinPart);
         r.wgs = parts < eva::kPagedWgs ? parts : eva::kPagedWgs;
     }
     return EVA_OK;
@@ -1414,6 +1414,7 @@ int eva_paged_decode(const eva_pcache* cache, const eva_page_table* table, const
     p.n_hg = r.n_hg;
     p.rows = (int)r.rows;
     p.wgs = (int)r.wgs;
+    p.f_wgs = eva::FastDiv(p.wgs > 0 ? p.wgs : 1);
     p.f_unit = eva::FastDiv(cache->H_kv * r.n_hg);
     p.f_hg = eva::FastDiv(r.n_hg);
     p.f_H = eva::FastDiv(cache->H);

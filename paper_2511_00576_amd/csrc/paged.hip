@@ -13,9 +13,9 @@
 //
 // The batch's rows may differ in length by any factor, and their lengths are on
 // the device.  So the launch has a fixed number of workgroups, and they share the
-// chunks of all rows, one row after the other, in equal contiguous parts: a
-// workgroup finds its part from the sequences' token counts (a scan, half a microsecond),
-// and rows that lie in more than one part are joined by a second launch.  Where rows are
+// chunks of all rows in equal parts, each within a row where the workgroups suffice for that,
+// else one row after the other: a workgroup finds its part from the sequences' token counts
+// (a scan, half a microsecond), and rows in more than one part are joined by a second launch.  Where rows are
 // short and many, every wave takes rows of its own, whole ones: no barrier, no joining.
 #include "paged.hpp"
 
@@ -330,41 +330,80 @@ void paged_decode_kernel(PagedParams a) {
         chunk_of = from + lane < a.t.B ? row_chunks<16 * NB>(a, i, tokens) : 0;
     };
     if (a.ws) {
-        window(0);
-        int chunks = chunk_of, longest = chunk_of, rows = chunk_of > 0;
-        for (int i = 64; i < a.t.B; i += 64) {
-            const int more = i + lane < a.t.B ? row_chunks<16 * NB>(a, i + lane, held_tokens(a.t, i + lane)) : 0;
-            chunks += more;
-            longest = max(longest, more);
-            rows += more > 0;
+        // all sequences: chunks, how many take part, whether a row is longer than a wave takes alone
+        int chunks = 0, active = 0, i = 0;
+        unsigned long long longer = 0, longest = 0;
+        do {
+            window(i);
+            chunks += chunk_of;
+            active += __builtin_popcountll(__builtin_amdgcn_ballot_w64(chunk_of > 0));
+            longer |= __builtin_amdgcn_ballot_w64(chunk_of > kPagedShortest);
+            longest |= __builtin_amdgcn_ballot_w64(chunk_of > kPagedShort);
+            i += 64;
+        } while (i < a.t.B);
+        int total = __builtin_amdgcn_readlane(wave_scan(chunks), 63) * unit;
+        alone = (active * unit >= kPagedMany ? longest : longer) == 0;
+        // What the workers are given in their order: rows (alone); parts of `part` chunks, each
+        // within one row (within), if that takes no more workgroups than there are; else
+        // chunks, whatever their row.  (A second row costs a workgroup 4 us: one sequence of 8000
+        // tokens 15.1 us against 13.8, so it is looked at for parts of up to kPagedWithin.)
+        bool within = false;
+        float inv = 0.f;
+        auto parts_of = [&](int x) {  // exact: x stays below 2^24 / kPagedWithin where it is asked
+            const int q = (int)((float)(x + part - 1) * inv);
+            return q - (q * part > x + part - 1) + ((q + 1) * part <= x + part - 1);
+        };
+        int workers = a.wgs, me = blockIdx.x;
+        if (alone) {
+            total = active * unit;
+            workers = a.wgs * NW;
+            me = me * NW + wave;
+        } else {
+            part = max((total + a.wgs - 1) / a.f_wgs, kPagedMinPart);
+            if (part <= kPagedWithin) {
+                inv = 1.f / (float)part;
+                int parts = 0;
+                if (a.t.B <= 64) {
+                    parts = parts_of(chunk_of);
+                } else {
+                    for (i = 0; i < a.t.B; i += 64) {
+                        window(i);
+                        parts += parts_of(chunk_of);
+                    }
+                }
+                parts = __builtin_amdgcn_readlane(wave_scan(parts), 63) * unit;
+                within = parts <= a.wgs;
+                if (within) total = parts;
+            }
         }
-        rows = __builtin_amdgcn_readlane(wave_scan(rows), 63) * unit;
-        alone = __builtin_amdgcn_readlane(wave_max(longest), 63) <= (rows >= kPagedMany ? kPagedShort : kPagedShortest);
-        const int total = alone ? rows : __builtin_amdgcn_readlane(wave_scan(chunks), 63) * unit;
-        const int workers = alone ? a.wgs * NW : a.wgs, me = alone ? (int)blockIdx.x * NW + wave : (int)blockIdx.x;
-        part = max((total + workers - 1) / workers, alone ? 1 : kPagedMinPart);
-        const long long from = (long long)me * part;
+        const int share = within ? 1 : alone ? (total + workers - 1) / workers : part;
+        const long long from = (long long)me * share;
         if (from >= total) return;
-        todo = min(part, total - (int)from);
-        // the sequence that holds chunk (or row) `from`
-        int before = 0, at;
+        todo = min(share, total - (int)from);
+        // the sequence that holds `from`
+        if (a.t.B > 64) window(0);
+        int before = 0, at, each;
         while (true) {
-            const int mine = (alone ? chunk_of > 0 : chunk_of) * unit;
-            const int upto = before + wave_scan(mine);
+            const int mine = alone ? chunk_of > 0 : within ? parts_of(chunk_of) : chunk_of;
+            const int upto = before + wave_scan(mine * unit);
             const unsigned long long past = __builtin_amdgcn_ballot_w64(upto > (int)from);
             if (past) {
                 const int l = __builtin_ctzll(past);
                 b = w0 + l;
-                at = (int)from - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(mine, l));
+                each = __builtin_amdgcn_readlane(mine, l);
+                at = (int)from - (__builtin_amdgcn_readlane(upto, l) - each * unit);
                 break;
             }
             before = __builtin_amdgcn_readlane(upto, 63);
             if (w0 + 64 >= a.t.B) return;  // only where the counts change during the call
             window(w0 + 64);
         }
-        const int each = alone ? 1 : __builtin_amdgcn_readlane(chunk_of, b - w0);
         row = at / each;
         c0 = at - row * each;
+        if (within) {
+            c0 *= part;
+            todo = min(part, __builtin_amdgcn_readlane(chunk_of, b - w0) - c0);
+        }
     } else {
         alone = a.alone;
         const int r = alone ? (int)blockIdx.x * NW + wave : (int)blockIdx.x;

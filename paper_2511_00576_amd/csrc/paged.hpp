@@ -51,17 +51,6 @@ __device__ __forceinline__ I wave_scan(I x) {
     return x;
 }
 
-// Largest of the wave's values, none of them negative, in lane 63.
-__device__ __forceinline__ int wave_max(int x) {
-    x = max(x, dpp<0x111>(x));
-    x = max(x, dpp<0x112>(x));
-    x = max(x, dpp<0x114>(x));
-    x = max(x, dpp<0x118>(x));
-    x = max(x, dpp<0x142, 0xa>(x));
-    x = max(x, dpp<0x143, 0xc>(x));
-    return x;
-}
-
 // Inclusive sum over the workgroup's threads, and the whole sum; sums has room for
 // every wave's.
 template <typename I>
@@ -110,7 +99,8 @@ struct PagedParams {
     int S, H, Hkv, G;
     int n_hg;           // groups of 16 paged_tiles(G) query heads of a kv head
     int rows;           // B Hkv n_hg
-    int wgs;            // workgroups that share all rows' chunks (with ws)
+    int wgs;            // workgroups of the launch (with ws)
+    FastDiv f_wgs;      // divisor of wgs
     int alone;          // without ws: a wave per row, not a workgroup
     FastDiv f_unit, f_hg;  // divisors of Hkv n_hg and of n_hg
     FastDiv f_H, f_G;      // of H and of G
@@ -132,12 +122,13 @@ constexpr int kPagedMinPart = 4;
 // Where no row can have more than kPagedMinPart chunks there is a workgroup per row, and a wave
 // per row from kPagedMany on (1 chunk: 512 rows 4.8 / 4.8, 1024 4.9 / 7.2, 4096 14.7 / 22.7).
 constexpr int kPagedShortest = 2, kPagedShort = 8, kPagedMany = 1024;
-// Workgroups that share a decode's chunks: as many as the CUs hold at once.
-constexpr int kPagedWgs = 512;
 // Tiles of 16 query heads that a workgroup has at once: with two, what a kv head's more than
 // 16 heads read is read once for 32 of them (20 heads, 256 sequences of up to 4096 tokens, 2 kv
 // heads, 720 MB: 139 us against 236).
 constexpr int paged_tiles(int G) { return G > 16 ? 2 : 1; }
+// Workgroups that share a decode's chunks: two a CU saturate the memory (64 sequences at 8k
+// 218 us; 257 with one and a half, 220 with three), and parts that end with their rows.
+constexpr int kPagedWgs = 512, kPagedWithin = 64;
 // Floats of a column of a share (paged.hip).
 __host__ __device__ constexpr int share_col(int d) { return d + 4; }
 // Bytes of the workspace: a pair of ints per row, then two shares per workgroup.
