@@ -245,6 +245,21 @@ def test_decode_shares_long_rows(P, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("B,H,Hkv", [(90, 8, 8), (270, 40, 2), (1100, 1, 1)])
+def test_more_rows_than_workgroups(B, H, Hkv, dtype):
+    # a workgroup's part begins and ends inside rows and holds several; a row of many workgroups among them
+    lens = [4000 if i == B // 2 else 330 if i % 3 else (i * 37) % 300 for i in range(B)]
+    cache, ks, vs = build(B, H, Hkv, 64, 32, lens, dtype, seed=B)
+    q = query(B, H, 64, dtype, seed=B)
+    active = [int(i % 7 != 2) for i in range(B)]
+    out = torch.full((B, H, 64), 3.0, dtype=dtype, device="cuda")
+    o = eva.paged_decode(cache, q.cuda(), active=ints(active), out=out)
+    skip = [b for b in range(B) if not active[b]]
+    check_rows(o, q, ks, vs, 32, dtype, skip=skip)
+    assert (o[skip] == 3).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("B,H,Hkv,longest,most", [
     (6, 6, 3, 32, 5000),       # rows so short that a wave takes each
     (150, 16, 8, 120, 5000),   # many rows, of up to eight chunks
