@@ -175,7 +175,7 @@ __global__ __launch_bounds__(kTableThreads) void page_truncate_kernel(PageTableV
 // keys go from registers to their rows and into the sums; values pass through LDS,
 // from which a lane takes the eight slots of a feature, the tiles' 16 bytes.  Rows
 // without a slot (a shorter sequence's padding) are not read.  Bound by memory for prompts
-// (three prompts of up to 4096 tokens, 8 kv heads, d = 128: 80 MB in 16 us, 5.0 TB/s; 18 with
+// (three prompts of up to 4096 tokens, 8 kv heads, d = 128: 80 MB in 15 us, 5.3 TB/s; 18 with
 // stores that keep their lines in the L2, 19 with 64 rows at a time, whose reads and
 // writes overlap less), by the chain slot -> row -> store for single tokens (64
 // sequences 3.7 us).
@@ -248,7 +248,7 @@ __global__ __launch_bounds__(kAppendThreads) void paged_append_kernel(PagedAppen
             const int r = r0 + p * RPT + my_row;
             if (r >= have && r < end && sh_slot[r] >= 0) {
                 const int s = sh_slot[r];
-                *reinterpret_cast<u32x4*>(kp + page_at(s) + (size_t)(s & mask) * D + piece) = kx[p];
+                __builtin_nontemporal_store(kx[p], reinterpret_cast<u32x4*>(kp + page_at(s) + (size_t)(s & mask) * D + piece));
                 add(kx[p]);
                 *reinterpret_cast<u32x4*>(&tile[r - r0][piece]) = vx[p];
             }
