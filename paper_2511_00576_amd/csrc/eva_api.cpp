@@ -1296,23 +1296,24 @@ eva::PageTableView table_of(const eva_page_table* t) {
     return eva::PageTableView{t->B, page_shift(t->P), t->n_pages, t->max_pages, t->n_tok, t->table, t->free_pages, t->n_free};
 }
 
-// Rows of a decode and the workgroups that share them; one per row where no row
-// has more chunks than a workgroup takes anyway.
+// Rows of a decode and the workgroups that share them.
 struct PagedRoute {
-    long long rows, wgs;  // wgs = 0: one per row
+    long long rows, wgs;  // wgs = 0: one per row, or (alone) a wave per row
     int n_hg;
+    bool alone;
 };
 int paged_route(PagedRoute& r, const eva_pcache* c, const eva_page_table* t, int S) {
     const int G = c->H / c->H_kv, per = 16 * eva::paged_tiles(G);
     r.n_hg = (int)(((long long)G + per - 1) / per);
     r.rows = (long long)t->B * c->H_kv * r.n_hg;
     const long long pages = S > 0 && S < t->max_pages ? S : t->max_pages;
-    const int tokens = 16 * eva::paged_blocks(c->d, c->dtype == EVA_F32 ? 4 : 2);
+    const int bytes = c->dtype == EVA_F32 ? 4 : 2, tokens = 16 * eva::paged_blocks(c->d, bytes);
     const long long chunks = (pages * t->P + tokens - 1) / tokens;
     // (threads of a launch stay below 2^32)
     if (r.rows * chunks > kMaxLen || (long long)t->B * c->H > 0xffffff) return EVA_ERR_UNSUPPORTED;
     r.wgs = 0;
-    if (chunks > eva::kPagedMinPart) {
+    r.alone = r.rows >= eva::kPagedMany && chunks <= eva::kPagedShort;
+    if (!eva::paged_whole(r.rows, chunks * tokens * c->d * 2 * bytes)) {
         const long long parts = r.rows * ((chunks + eva::kPagedMinPart - 1) / eva::kPagedMinPart);
         r.wgs = parts < eva::kPagedWgs ? parts : eva::kPagedWgs;
     }
@@ -1422,7 +1423,7 @@ int eva_paged_decode(const eva_pcache* cache, const eva_page_table* table, const
     p.scale_log2 = (float)(1.4426950408889634 / sqrt((double)cache->d));
     if (r.wgs > 0 && ws && aligned16(ws) && ws_bytes >= eva::paged_ws_bytes(r.rows, r.wgs, cache->d, p.G))
         p.ws = static_cast<float*>(ws);
-    p.alone = r.wgs == 0 && r.rows >= eva::kPagedMany;
+    p.alone = r.wgs == 0 && r.alone;
     hipStream_t s = static_cast<hipStream_t>(stream);
     return hip_status(dispatch(cache->d, cache->dtype, [&](auto dd, auto t) {
         return eva::launch_paged_decode<decltype(dd)::value, decltype(t)>(p, s);

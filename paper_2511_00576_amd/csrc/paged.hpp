@@ -119,8 +119,9 @@ constexpr int kPagedMinPart = 4;
 //      512   7.1 / 12.6  8.1 / 9.4   12.8 / 9.9  21 / 15
 //     1024   8.1 / 13.7  10.5 / 12.2 15.6 / 15.7 26.2 / 26.6
 //     4096   24 / 33     33 / 40     53 / 58     92 / 99
-// Where no row can have more than kPagedMinPart chunks there is a workgroup per row, and a wave
-// per row from kPagedMany on (1 chunk: 512 rows 4.8 / 4.8, 1024 4.9 / 7.2, 4096 14.7 / 22.7).
+// Where rows can have no more than kPagedShort chunks at all and paged_whole() gives each
+// its workgroup, a wave takes it from kPagedMany on (1 chunk: 512 rows 4.8 / 4.8, 1024 4.9 /
+// 7.2, 4096 14.7 / 22.7).
 constexpr int kPagedShortest = 2, kPagedShort = 8, kPagedMany = 1024;
 // Tiles of 16 query heads that a workgroup has at once: with two, what a kv head's more than
 // 16 heads read is read once for 32 of them (20 heads, 256 sequences of up to 4096 tokens, 2 kv
@@ -129,6 +130,17 @@ constexpr int paged_tiles(int G) { return G > 16 ? 2 : 1; }
 // Workgroups that share a decode's chunks: two a CU saturate the memory (64 sequences at 8k
 // 218 us; 257 with one and a half, 220 with three), and parts that end with their rows.
 constexpr int kPagedWgs = 512, kPagedWithin = 64;
+// Whether every row, of `bytes` of keys and values at most, is left to one workgroup, which
+// saves the second launch.  us in a replayed graph, shared / one each, rows of the same length
+// in chunks of 16 KB:
+//     rows   8 chunks     12           16           24           48
+//        8   8.7 / 6.0    8.9 / 7.1    8.8 / 8.2    8.9 / 10.3   8.9 / 17.2
+//       64   8.9 / 6.7    9.4 / 8.9    9.5 / 11.2   11.1 / 15.2  14.4 / 27.2
+//      192                                          20.7 / 19.8  31.2 / 31.3
+//      256   11.9 / 8.0   14.6 / 10.6  16.6 / 13.1  21.7 / 18.3  36.7 / 33.5
+//     1024   26.2 / 22.1  37.0 / 31.9  46.6 / 41.9  67.7 / 61.4  124 / 120
+// (300 rows of 96 chunks 80 / 104: from 48 on it is a matter of how rows fit the CUs.)
+inline bool paged_whole(long long rows, long long bytes) { return bytes <= (rows >= 192 ? 24 : 12) * 16384; }
 // Floats of a column of a share (paged.hip).
 __host__ __device__ constexpr int share_col(int d) { return d + 4; }
 // Bytes of the workspace: a pair of ints per row, then two shares per workgroup.

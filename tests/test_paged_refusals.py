@@ -119,7 +119,11 @@ def test_workspaces(lib):
     assert lib.eva_paged_select_workspace_bytes(ref(c), ref(LONG), 5) == 2 * 2 * 2000 * 8
     assert lib.eva_paged_select_workspace_bytes(ref(c), ref(t), 5) == 0
     assert lib.eva_paged_decode_workspace_bytes(ref(c), ref(t), 0) > 0
-    assert lib.eva_paged_decode_workspace_bytes(ref(c), ref(t), 1) == 0       # two chunks a row: one workgroup each
+    # rows of 12 blocks of 16 KB of keys and values, and of one more: 768 tokens of 64 features
+    assert lib.eva_paged_decode_workspace_bytes(ref(c), ref(t), 12) == 0
+    assert lib.eva_paged_decode_workspace_bytes(ref(c), ref(t), 13) > 0
+    assert lib.eva_paged_decode_workspace_bytes(ref(c), ref(table(B=100)), 24) == 0   # twice that from 192 rows on
+    assert lib.eva_paged_decode_workspace_bytes(ref(c), ref(table(B=100)), 25) > 0
     assert lib.eva_paged_decode_workspace_bytes(ref(c), ref(t), -1) == 0
 
 
