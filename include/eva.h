@@ -786,9 +786,9 @@ int eva_paged_append(const eva_pcache* cache, const void* k_new, const void* v_n
  * are left as they were.  A row that meets an entry of the table outside the pool is NaN.
  * o may not overlap q.
  * ws: optional device scratch of eva_paged_decode_workspace_bytes() bytes, which
- * every call that overlaps another needs for its own: the chunks of 32 tokens of all
- * rows are shared evenly by the workgroups, and rows that several of them had are
- * joined by a second launch; with less, a workgroup takes each row.
+ * every call that overlaps another needs for its own: the keys of all rows are shared
+ * evenly by the workgroups, and rows that several of them had are joined by a second
+ * launch; with less, or where rows cannot be long (0 bytes), a workgroup takes each row.
  * The same call gives the same bits; the order of a row's sum depends on all lengths.
  * Errors: INVALID (malformed or different table and cache, null or misaligned
  * pointers, S), UNSUPPORTED (d, dtype, sizes).
