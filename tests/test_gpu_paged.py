@@ -349,8 +349,8 @@ def test_values_that_are_not_finite(n, use_workspace, dtype):
     assert o[1].isnan().all() and (o[2] == INF).all() and o[3].isnan().all() and o[4].isnan().all()
     odd = list(range(1, n, 2))
     ref, bound = attend(q[5], ks[5][odd, 0].double(), vs[5][odd, 0].double(), dtype)
-    # a wave or share of -inf alone has no weight; the bound counts the keys that the sum runs over
-    assert ((o[5] - ref).abs() <= 2 * bound).all()
+    # (weights of 0 add nothing, exactly)
+    assert ((o[5] - ref).abs() <= bound).all()
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
@@ -545,9 +545,10 @@ def test_prompt_generation_and_rollback(dtype):
     last = torch.stack([q[b, :, n - 1] for b, n in enumerate(lens)])
     o = eva.paged_decode(cache, last.cuda())
     check_rows(o, last, ks, vs, P, dtype)
-    # (the prefill's bf16 weights are rounded once, 2^-8 of the absolute values' sum)
+    # apart by each side's output rounding and by the prefill's rounded weights: 2^-8 of the largest value
+    # each, and 2^-15 for the decode's weights
     same = torch.stack([whole[b, :, n - 1] for b, n in enumerate(lens)])
-    assert (same.double() - o.double()).abs().max() <= 2.0 ** -7 * max(float(v[b].abs().max()) for b in range(B)) * 2
+    assert (same.double() - o.double()).abs().max() <= (3 * 2.0 ** -8 + 2.0 ** -14) * float(v.abs().max())
     for s in range(steps):
         if s == 10:
             back([0, len(ks[1]), len(ks[2])])
