@@ -780,8 +780,9 @@ int eva_paged_append(const eva_pcache* cache, const void* k_new, const void* v_n
  * with pages (device int32 [B][H_kv][S], as eva_paged_select gives them; NULL: S =
  * 0), over those in the first min(S, pages held) listed pages of the kv head, each as
  * often as it stands there (entries that are none of the sequence's pages: nothing).
- * Sums are fp32; softmax weights of bf16 rows are held in 16 bits (two bf16 numbers) for
- * the products with the values, and the output is rounded once.
+ * Sums are fp32; softmax weights of bf16 rows are held in 16 bits (two bf16 numbers), and
+ * to 2^-126 at least, for the products with the values, and the output is rounded once.
+ * A weight below 2^-126 of the largest may count as 0, under which an infinite value gives NaN.
  * A row without keys is zeros.  Rows of sequences that are not active (device int32 [B], 0; NULL: all are)
  * are left as they were.  A row that meets an entry of the table outside the pool is NaN.
  * o may not overlap q.

@@ -185,8 +185,14 @@ struct Chunk<D, bf16> {
     // Weights as the products' operand: two bf16 numbers each, the weight cut off after 8
     // bits and what that left, 16 bits in all (one rounded number would double the square of
     // the output's error, 0.0017 -> 0.0023 of its norm with the output's own rounding).  The
-    // second product is hidden behind memory: 217.8 us for 64 sequences at 8k either way.  What
-    // is left is never 0, so that an infinite value keeps its sign and times it is no NaN.
+    // second product is hidden behind memory: 217.8 us for 64 sequences at 8k either way.
+    //
+    // What is left is not 0 under a weight that is not, since an infinite value times 0 is NaN: it is
+    // 2^-126 at least, bf16's smallest normal number and the smallest weight that exp2 gives
+    // (those below are 0), or the weight itself if that is less.
+    static __device__ __forceinline__ float rest(float x, uint32_t xu) {
+        return fmaxf(x - __uint_as_float(xu & 0xffff0000u), fminf(x, 0x1p-126f));
+    }
     __device__ __forceinline__ void add(const floatx4 (&p)[2], floatx4 (&acc)[D / 16]) const {
         u32x4 hi, lo;
 #pragma unroll
@@ -194,8 +200,7 @@ struct Chunk<D, bf16> {
             const float x = p[i / 2][i % 2 * 2], y = p[i / 2][i % 2 * 2 + 1];
             const uint32_t xu = __float_as_uint(x), yu = __float_as_uint(y);
             hi[i] = __builtin_amdgcn_perm(yu, xu, 0x07060302);
-            lo[i] = pack_bf16x2(fmaxf(x - __uint_as_float(xu & 0xffff0000u), x * 0x1p-30f),
-                                fmaxf(y - __uint_as_float(yu & 0xffff0000u), y * 0x1p-30f));
+            lo[i] = pack_bf16x2(rest(x, xu), rest(y, yu));
         }
 #pragma unroll
         for (int i = 0; i < D / 16; ++i)

@@ -1,0 +1,53 @@
+"""The paged cache where numbers and tables are at their limits: infinite values under the
+smallest weights, scores of any magnitude, pages that the pool does not have."""
+import math
+
+import pytest
+import torch
+
+from paper_2511_00576_amd import eva
+from test_gpu_paged import BF16, F32, INF, build, ints
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU visible")
+    eva._lib.load()
+
+
+def place(cache, b, pos):
+    """Page and place of a position."""
+    P = cache.struct.P
+    return int(cache.table.table[b, pos // P]), pos % P
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("use_workspace", [True, False])
+@pytest.mark.parametrize("n", [20, 4000])
+@pytest.mark.parametrize("below", [60, 66, 70, 74, 78, 82, 86, 87])
+def test_an_infinite_value_under_a_small_weight_is_infinite(below, n, use_workspace, dtype):
+    """All scores are 0 but one, `below` under them: its weight, e^-below of the others' and 2^-126 or more
+    (87 / ln 2 = 125.5), is not 0, and times an infinite value that is infinite."""
+    P, d, pos = 32, 64, n - 7
+    cache, ks, vs = build(1, 2, 1, d, P, [n], dtype, seed=5)
+    cache.k[cache.table.table[0, :-(-n // P)].long()] = 0.0
+    page, off = place(cache, 0, pos)
+    cache.k[page, 0, off, 0] = -float(below)          # q . k / sqrt(64) = -below
+    cache.vt[page, 0, off // 8, :16, off % 8] = INF
+    cache.vt[page, 0, off // 8, 16:32, off % 8] = -INF
+    q = torch.zeros(1, 2, d, dtype=dtype)
+    q[:, :, 0] = 8.0
+    o = eva.paged_decode(cache, q.cuda(), use_workspace=use_workspace)[0].cpu().double()
+    assert (o[:, :16] == INF).all() and (o[:, 16:32] == -INF).all()
+    # the other features: the mean of the other rows, by weights of 1 exactly, of which n are summed one by one
+    # at worst, and divided; the row's own part is e^-60 or less.  bf16's output is rounded, half a step
+    rest = [p for p in range(n) if p != pos]
+    v = vs[0][rest, 0, 32:].double()
+    bound = (2 * n + 4) * 2.0 ** -24 * v.abs().mean(0) + math.exp(-60) * float(vs[0].abs().max())
+    if dtype == BF16:
+        # (a weight of 1 is off by 2^-30, what is left of it)
+        bound = bound + 2.0 ** -8 * v.mean(0).abs() + 2.0 ** -29 * v.abs().mean(0)
+    assert ((o[:, 32:] - v.mean(0)).abs() <= bound).all()
