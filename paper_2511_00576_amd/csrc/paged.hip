@@ -98,7 +98,11 @@ struct RowState {
         for (int i = 0; i < D / 16; ++i) acc[i] = floatx4{0.f, 0.f, 0.f, 0.f};
     }
     // Scores of a chunk (two blocks of four per lane) become weights; the reference
-    // maximum moves only when the chunk's exceeds it by more than kPagedTau.
+    // maximum moves only when the chunk's exceeds it by more than kPagedTau.  The maximum is one of
+    // the scores as they are and is taken off before they are scaled, so that it weighs 1 exactly:
+    // scaled and rounded first it would be off by half a step, 128 from 2^31 on, and the weights
+    // infinite or 0.  (One instruction a score more than a fused scaling: 64 sequences at 8k 218.8
+    // us against 218.7, 1024 rows of 64 to 512 tokens 0 to 1%.)
     template <int NB>
     __device__ __forceinline__ void weigh(floatx4 (&s)[NB], float scale) {
         float mx = s[0][0];
@@ -106,23 +110,23 @@ struct RowState {
         for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
             for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[kb][i]);
-        mx = xgroup_max(mx) * scale;
-        const bool raise = mx > m + kPagedTau;
+        mx = xgroup_max(mx);
+        const bool raise = (mx - m) * scale > kPagedTau;
         if (__builtin_amdgcn_ballot_w64(raise)) {
             const float next = raise ? mx : m;
-            const float alpha = raise ? fast_exp2(m - next) : 1.f;  // the first time: exp2(-inf) = 0
+            const float alpha = raise ? fast_exp2((m - next) * scale) : 1.f;  // the first time: exp2(-inf) = 0
             l *= alpha;
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) acc[i] *= alpha;
             m = next;
         }
         // no maximum yet (scores of -inf alone): their weights are 0
-        const float off = m == -INFINITY ? 0.f : -m;
+        const float off = m == -INFINITY ? 0.f : m;
 #pragma unroll
         for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                s[kb][i] = fast_exp2(fmaf(s[kb][i], scale, off));
+                s[kb][i] = fast_exp2((s[kb][i] - off) * scale);
                 l += s[kb][i];
             }
     }
@@ -532,7 +536,7 @@ void paged_decode_kernel(PagedParams a) {
                     // without a maximum there is no weight; sums of NaN stay, and where there is none at
                     // all the waves' reasons are summed as they are
                     const float mw = red_m[w][col];
-                    const float wt = m == -INFINITY ? 1.f : mw == -INFINITY ? 0.f : fast_exp2(mw - m);
+                    const float wt = m == -INFINITY ? 1.f : mw == -INFINITY ? 0.f : fast_exp2((mw - m) * a.scale_log2);
                     sum += wt * red_l[w][col];
                     o += wt * *reinterpret_cast<const floatx4*>(&red_o[w][col][f]);
                 }
@@ -575,18 +579,18 @@ struct Joined {
     float m = -INFINITY, l = 0.f;
     floatx4 o = {0.f, 0.f, 0.f, 0.f};
     template <int N>
-    __device__ __forceinline__ void add(const float (&mx)[N], const float (&lx)[N], const floatx4 (&ox)[N]) {
+    __device__ __forceinline__ void add(const float (&mx)[N], const float (&lx)[N], const floatx4 (&ox)[N], float scale) {
         float top = m;
 #pragma unroll
         for (int i = 0; i < N; ++i) top = fmaxf(top, mx[i]);
         // without a maximum there is no weight; sums of NaN stay, and where there is none at
         // all the reasons (finish()) are summed as they are
-        const float keep = top == -INFINITY ? 1.f : m == -INFINITY ? 0.f : fast_exp2(m - top);
+        const float keep = top == -INFINITY ? 1.f : m == -INFINITY ? 0.f : fast_exp2((m - top) * scale);
         l *= keep;
         o *= keep;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const float wt = top == -INFINITY ? 1.f : mx[i] == -INFINITY ? 0.f : fast_exp2(mx[i] - top);
+            const float wt = top == -INFINITY ? 1.f : mx[i] == -INFINITY ? 0.f : fast_exp2((mx[i] - top) * scale);
             l += wt * lx[i];
             o += wt * ox[i];
         }
@@ -631,7 +635,7 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedParams a)
                 l[i] = 0.f;
                 o[i] = floatx4{0.f, 0.f, 0.f, 0.f};
             }
-        j.add(m, l, o);
+        j.add(m, l, o, a.scale_log2);
     }
     if (f == 0) {
         red_m[grp] = j.m;
@@ -649,7 +653,7 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedParams a)
         o[i] = red_o[i][f / 4];
     }
     Joined<D> all;
-    all.add(m, l, o);
+    all.add(m, l, o, a.scale_log2);
     store4(static_cast<T*>(a.o) + (size_t)blockIdx.x * D + f, finish(all.m, all.l, all.o));
 }
 

@@ -51,3 +51,37 @@ def test_an_infinite_value_under_a_small_weight_is_infinite(below, n, use_worksp
         # (a weight of 1 is off by 2^-30, what is left of it)
         bound = bound + 2.0 ** -8 * v.mean(0).abs() + 2.0 ** -29 * v.abs().mean(0)
     assert ((o[:, 32:] - v.mean(0)).abs() <= bound).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("use_workspace", [True, False])
+@pytest.mark.parametrize("n", [20, 3000])
+@pytest.mark.parametrize("power", [3, 13, 14, 16, 20, 40])
+def test_scores_of_any_magnitude(power, n, use_workspace, dtype):
+    """Queries and keys of small whole numbers times 2^power: products and their sums (64 times 64 at most) are exact
+    in fp32, and from 2^13 on two different scores differ by 2^26 / 8 or more, so that a row is the mean of the values
+    of its highest scores: of t of them, t additions and a division, u each.  2^3: by 8 or more, all weights count."""
+    P, d, G = 32, 64, 2
+    cache, ks, vs = build(2, G, 1, d, P, [n, n // 2 + 1], dtype, seed=power)
+    g = torch.Generator().manual_seed(power)
+    q = torch.randint(-8, 9, (2, G, d), generator=g)
+    q[:, :, 0] += (q == 0).all(-1)
+    small = torch.randint(-8, 9, cache.k.shape, generator=g)
+    cache.k.copy_(torch.ldexp(small.double(), torch.tensor(power)).to(dtype))
+    table = cache.table.table.cpu().long()
+    o = eva.paged_decode(cache, torch.ldexp(q.double(), torch.tensor(power)).to(dtype).cuda(),
+                         use_workspace=use_workspace).cpu().double()
+    for b, m in enumerate((n, n // 2 + 1)):
+        k = small[table[b], 0].reshape(-1, d)[:m]
+        score = torch.ldexp((q[b] @ k.T).double() / 8, torch.tensor(2 * power))
+        p = torch.softmax(score, -1)
+        v = vs[b][:, 0].double()
+        want, size = p @ v, p @ v.abs()
+        ties = int((p > 0).sum(-1).max())
+        bound = (2 * ties + 8) * 2.0 ** -24 * size
+        if power == 3:   # logits of up to 2^6 2^9 / 8 = 4096: 4 u of that in a weight of the numerator and of the denominator
+            bound = bound + 8 * 4096 * 2.0 ** -24 * (size + want.abs())
+        if dtype == BF16:
+            bound = bound + 2.0 ** -8 * want.abs() + 2.0 ** -15 * size
+        assert torch.isfinite(o[b]).all()
+        assert ((o[b] - want).abs() <= bound).all()
