@@ -722,7 +722,8 @@ typedef struct eva_page_table {
  * need pages too: they do not overtake it.)  New pages are taken from the top of
  * the stack in the order of (sequence, page) and entered in the table,
  * n_tok[b] += granted[b], and
- *     slots[b][i] = slot of the token at position n + i for i < granted[b], else -1
+ *     slots[b][i] = slot of the token at position n + i for i < granted[b] (-1 in a page
+ *                   that the pool does not have), else -1
  *     start[b]    = n, the position of the first one (eva_qk_norm_rope's `start`)
  * slots [B][T], start, granted [B]: device int32.  Nothing else is changed.
  * Errors: INVALID (malformed table, T < 1, null or misaligned pointers),

@@ -22,6 +22,12 @@ constexpr int kFewTokens = 16;
 // Slots that a workgroup of that launch writes.
 constexpr int kSlotTile = 1024;
 
+// Slot of place `off` of a page, -1 where the pool does not have it (page << shift could pass 2^32
+// and come back inside).
+__device__ __forceinline__ int slot_of(const PageTableView& t, int page, int off) {
+    return (unsigned)page < (unsigned)t.n_pages ? page << t.shift | off : -1;
+}
+
 __global__ __launch_bounds__(kTableThreads) void page_extend_kernel(PageTableView t, const int* __restrict__ counts, int T,
                                                                     int* __restrict__ slots, int* __restrict__ start,
                                                                     int* __restrict__ granted) {
@@ -59,7 +65,7 @@ __global__ __launch_bounds__(kTableThreads) void page_extend_kernel(PageTableVie
                 if (need > 0) pages[held] = fresh;
                 for (int i = 0; i < T; ++i) {
                     const int p = n + i;
-                    row[i] = i < c ? ((p >> t.shift) < held ? last : fresh) << t.shift | (p & mask) : -1;
+                    row[i] = i < c ? slot_of(t, (p >> t.shift) < held ? last : fresh, p & mask) : -1;
                 }
             } else {
                 // the tiles of the second launch find it in their first slot
@@ -95,7 +101,7 @@ __global__ __launch_bounds__(256) void page_slots_kernel(PageTableView t, int T,
         if (i < c) {
             const int p = n + i, lp = p >> t.shift;
             const int page = lp < held ? pages[lp] : t.free_pages[top - (lp - held)];
-            s = page << t.shift | (p & mask);
+            s = slot_of(t, page, p & mask);
             if (lp >= held && (p & mask) == 0) pages[lp] = page;
         }
         row[i] = s;

@@ -85,3 +85,37 @@ def test_scores_of_any_magnitude(power, n, use_workspace, dtype):
             bound = bound + 2.0 ** -8 * want.abs() + 2.0 ** -15 * size
         assert torch.isfinite(o[b]).all()
         assert ((o[b] - want).abs() <= bound).all()
+
+
+@pytest.mark.parametrize("T", [3, 40])
+@pytest.mark.parametrize("P", [16, 64])
+def test_a_page_that_the_pool_does_not_have_has_no_slots(P, T):
+    """Entries so far outside that page times P passes 2^32 and would lie inside: neither the page that a sequence
+    has, nor one from the stack of free pages, gives a slot."""
+    N, far = 6, 2 ** 32 // P
+    t = eva.PageTable(4, P, N, 8 * P)
+    t.n_tok.copy_(ints([P + 2, P - 1, 0, 5]))
+    t.table[0, :2] = ints([0, far + 1])      # its second page, which is being filled
+    t.table[1, 0] = 1
+    t.table[3, 0] = -7
+    t.free_pages[:4] = ints([2, 3, -1, far + 4])
+    t.n_free.fill_(4)
+    slots, start, granted = eva.page_extend(t, T, ints([1, T, 0, 2]))
+    assert granted.tolist() == [1, T, 0, 2] and start.tolist() == [P + 2, P - 1, 0, 5]
+    s = slots.tolist()
+    assert s[0] == [-1] * T and s[2] == [-1] * T and s[3] == [-1] * T
+    # the second sequence: the last place of page 1, then a page from far outside, then -1, then page 3
+    assert s[1][0] == P + P - 1
+    new = [p // P for p in range(P, P + T - 1)]
+    stack = [far + 4, -1, 3, 2]
+    want = [stack[j - 1] * P + p % P if 0 <= stack[j - 1] < N else -1 for p, j in zip(range(P, P + T - 1), new)]
+    assert s[1][1:] == want
+    assert t.table[1, 1].item() == far + 4
+    # nothing is written for them, and the rows that meet such a page are NaN
+    cache = eva.PagedCache(t, 2, 1, 64, fill=0.0)
+    x = torch.ones(4, 1, T, 64, dtype=BF16, device="cuda")
+    eva.paged_append(cache, x, x, slots)
+    written = sum(i >= 0 for r in s for i in r)
+    assert cache.k.sum() == written * 64 and cache.vt.sum() == written * 64
+    o = eva.paged_decode(cache, torch.ones(4, 2, 64, dtype=BF16, device="cuda"))
+    assert o[0].isnan().all() and o[1].isnan().all() and (o[2] == 0).all() and o[3].isnan().all()
