@@ -793,7 +793,7 @@ int eva_paged_append(const eva_pcache* cache, const void* k_new, const void* v_n
  * launch; with less, or where rows cannot be long (0 bytes), a workgroup takes each row.
  * The same call gives the same bits; the order of a row's sum depends on all lengths.
  * Errors: INVALID (malformed or different table and cache, null or misaligned
- * pointers, S), UNSUPPORTED (d, dtype, sizes).
+ * pointers, S), UNSUPPORTED (d, dtype, S above 2^30, sizes).
  */
 int eva_paged_decode(const eva_pcache* cache, const eva_page_table* table, const void* q, void* o, const int* pages, int S,
                      const int* active, void* ws, size_t ws_bytes, void* stream);

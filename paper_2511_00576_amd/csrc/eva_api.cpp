@@ -1303,6 +1303,7 @@ struct PagedRoute {
     bool alone;
 };
 int paged_route(PagedRoute& r, const eva_pcache* c, const eva_page_table* t, int S) {
+    if (S > kMaxLen) return EVA_ERR_UNSUPPORTED;
     const int G = c->H / c->H_kv, per = 16 * eva::paged_tiles(G);
     r.n_hg = (int)(((long long)G + per - 1) / per);
     r.rows = (long long)t->B * c->H_kv * r.n_hg;
@@ -1362,7 +1363,7 @@ int eva_paged_append(const eva_pcache* cache, const void* k_new, const void* v_n
 }
 
 size_t eva_paged_select_workspace_bytes(const eva_pcache* cache, const eva_page_table* table, int S) {
-    if (check_paged(cache, table) != EVA_OK || S < 1 || eva::select_alone((long long)table->B * cache->H_kv, table->max_pages))
+    if (check_paged(cache, table) != EVA_OK || S < 1 || S > kMaxLen || eva::select_alone((long long)table->B * cache->H_kv, table->max_pages))
         return 0;
     return (size_t)table->B * cache->H_kv * table->max_pages * sizeof(unsigned long long);
 }
@@ -1374,6 +1375,7 @@ int eva_paged_select(const eva_pcache* cache, const eva_page_table* table, const
     if (S < 1 || first < 0 || last < 1 || (long long)first + last > S || !q || !pages || !cache->k_mean || !aligned16(q) ||
         !aligned4(pages))
         return EVA_ERR_INVALID;
+    if (S > kMaxLen) return EVA_ERR_UNSUPPORTED;  // places in a list, and past it, stay below 2^31
     const size_t need = eva_paged_select_workspace_bytes(cache, table, S);
     if (need && (!ws || !aligned16(ws))) return EVA_ERR_INVALID;
     if (ws_bytes < need) return EVA_ERR_CAPACITY;

@@ -1,0 +1,26 @@
+"""Sizes of the paged cache's calls beyond what the library, or its C interface's 32-bit numbers, can
+take are refused before memory is taken and before the GPU is touched (no compute call is made here)."""
+import pytest
+import torch
+
+from paper_2511_00576_amd import _lib, eva
+from test_paged_refusals import FAKE, INVALID, LONG, UNSUPPORTED, decode, host, lib, pool, ref, select, table  # noqa: F401
+
+LONGEST = 2 ** 30
+
+
+@pytest.mark.parametrize("S,first,last", [
+    (LONGEST + 1, 1, 1),
+    (2 ** 31 - 1, 0, 1),              # the loop over a list's entries would pass 2^31
+    (2 ** 31 - 1, 2 ** 31 - 2, 1),    # the first ranked page's place too
+    (2 ** 31 - 1, 2 ** 31 - 100, 99),
+])
+def test_long_lists(lib, S, first, last):  # noqa: F811
+    for t in (table(), LONG):
+        assert select(lib, t=t, S=S, first=first, last=last) == UNSUPPORTED
+        assert decode(lib, t=t, pages=FAKE, S=S) == UNSUPPORTED
+        assert lib.eva_paged_select_workspace_bytes(ref(pool()), ref(t), S) == 0
+        assert lib.eva_paged_decode_workspace_bytes(ref(pool()), ref(t), S) == 0
+    # a malformed call stays that
+    assert select(lib, S=S, first=S, last=1) == INVALID
+    assert decode(lib, pages=None, S=S) == INVALID
