@@ -721,6 +721,9 @@ def append_path(cache, k, v, path=None, counts=None, active=None):
 
 
 # ---- paged cache ---------------------------------------------------------------
+_LONGEST = 1 << 30  # tokens, slots and list entries; the C interface's ints would wrap beyond 2^31
+
+
 class PageTable:
     """Which pages of a pool the sequences of a batch have (see eva_page_table in
     eva.h), shared by all layers' PagedCaches: n_tok [B], table [B, max_pages],
@@ -733,6 +736,8 @@ class PageTable:
         if page not in (16, 32, 64, 128, 256):
             raise ValueError("a page holds 16, 32, 64, 128 or 256 tokens")
         rows = -(-max_tokens // page)
+        if max(B, B * rows, n_pages * page, rows * page) > _LONGEST:
+            raise ValueError("a table has up to 2^30 entries, its pool and each of its rows up to 2^30 tokens")
         if storage is None:
             self.n_tok = torch.zeros(B, dtype=torch.int32, device=device)
             self.table = torch.full((B, rows), -1, dtype=torch.int32, device=device)
@@ -759,6 +764,8 @@ class PagedCache:
 
     def __init__(self, table: PageTable, H, Hkv, d, dtype=torch.bfloat16, means=True, fill=None, storage=None):
         t, dev = table.struct, table.n_tok.device
+        if max(H, Hkv, d) > _LONGEST:
+            raise ValueError("H, Hkv and d are at most 2^30")
         shapes = ((t.n_pages, Hkv, t.P, d), (t.n_pages, Hkv, t.P // 8, d, 8), (t.n_pages, Hkv, d))
         if storage is None:
             mk = (lambda s, dt: torch.full(s, fill, dtype=dt, device=dev)) if fill is not None else \
@@ -787,8 +794,8 @@ def page_extend(table: PageTable, T: int = 1, counts=None):
     every sequence: (slots [B, T], start [B], granted [B]), int32.  A sequence that the
     free pages or its row of the table do not suffice for is granted none."""
     s, dev = table.struct, table.n_tok.get_device()
-    if T < 1:
-        raise ValueError("T must be at least 1")
+    if not 1 <= T <= _LONGEST:
+        raise ValueError("T must be at least 1 and at most 2^30")
     B, n_tok = s.B, table.n_tok
     c = _expect(counts, "counts", (B,), torch.int32, dev)
     slots, start = n_tok.new_empty((B, T)), torch.empty_like(n_tok)
@@ -824,8 +831,10 @@ def paged_select(cache: PagedCache, q, n_pages: int, first: int = 1, last: int =
     s, dev, t = cache.struct, cache.k.get_device(), cache.table
     B = t.struct.B
     pq = _expect(q, "q", (B, s.H, s.d), cache.dtype, dev)
-    if n_pages < 1:
-        raise ValueError("n_pages must be at least 1")
+    if not 1 <= n_pages <= _LONGEST:
+        raise ValueError("n_pages must be at least 1 and at most 2^30")
+    if first < 0 or last < 1 or first + last > n_pages:
+        raise ValueError("first must be at least 0, last at least 1, and both together at most n_pages")
     pages = t.n_tok.new_empty((B, s.H_kv, n_pages))
     n = cache._ws_bytes("eva_paged_select_workspace_bytes", n_pages)
     ws = _scratch(q, n)
@@ -845,6 +854,8 @@ def paged_decode(cache: PagedCache, q, pages=None, active=None, out=None, use_wo
         if pages.dim() != 3 or pages.shape[2] < 1:
             raise ValueError("pages must be [B, Hkv, S]")
         S = pages.shape[2]
+        if S > _LONGEST:
+            raise ValueError("a list of pages has at most 2^30 entries")
     pp = _expect(pages, "pages", (B, s.H_kv, S), torch.int32, dev)
     on = _expect(active, "active", (B,), torch.int32, dev)
     o, po = _rows_out(q, out, active is None, dev)
