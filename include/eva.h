@@ -722,8 +722,8 @@ typedef struct eva_page_table {
  * need pages too: they do not overtake it.)  New pages are taken from the top of
  * the stack in the order of (sequence, page) and entered in the table,
  * n_tok[b] += granted[b], and
- *     slots[b][i] = slot of the token at position n + i for i < granted[b] (-1 in a page
- *                   that the pool does not have), else -1
+ *     slots[b][i] = slot of the token at position n + i for i < granted[b] (in a page that
+ *                   the pool does not have: its place less P, which is negative), else -1
  *     start[b]    = n, the position of the first one (eva_qk_norm_rope's `start`)
  * slots [B][T], start, granted [B]: device int32.  Nothing else is changed.
  * Errors: INVALID (malformed table, T < 1, null or misaligned pointers),
@@ -763,7 +763,7 @@ typedef struct eva_pcache {
 /*
  * Write new tokens' rows into their slots: k_new, v_new [B][H_kv][T][d], slots
  * device int32 [B][T] as eva_page_extend gives them (tokens of one sequence in successive
- * places, then -1: those are not written, nor are slots outside the pool).  A page
+ * places, then -1: those are not written, nor are slots outside the pool, negative or not).  A page
  * whose last place is written gets its mean key, from all its keys as the pool holds
  * them, with the same bits however many calls filled it.  Where two sequences are
  * given the same slot either row may stay.

@@ -113,12 +113,23 @@ constexpr int paged_blocks(int d, int bytes) { return bytes == 4 && d == 128 ? 1
 constexpr int kPagedMinPart = 4;
 // Rows of up to kPagedShortest chunks go to one wave each, and of up to kPagedShort where
 // there are kPagedMany and more.  us in a replayed graph, a wave / a workgroup (which takes
-// kPagedMinPart chunks and more, however many rows that is), bf16 d = 128, chunks of 32 tokens:
-//     rows   1 chunk     2           4           8
-//      256   6.9 / 12.4  8.0 / 9.2   10.1 / 7.6  18.7 / 11.8
-//      512   7.1 / 12.6  8.1 / 9.4   12.8 / 9.9  21 / 15
-//     1024   8.1 / 13.7  10.5 / 12.2 15.6 / 15.7 26.2 / 26.6
-//     4096   24 / 33     33 / 40     53 / 58     92 / 99
+// kPagedMinPart chunks and more, however many rows that is), by the rows' chunks:
+//     rows   1 chunk      2            4            8
+//   bf16, d = 128: 32 tokens, 16 KB
+//      256   7.0 / 7.0    7.9 / 7.2    10.1 / 7.8   18.1 / 11.9
+//      512   7.1 / 7.6    8.2 / 8.2    12.9 / 9.9   20.9 / 14.8
+//     1024   8.2 / 14.1   10.7 / 12.7  16.0 / 16.2  25.7 / 27.2
+//     4096   24 / 36      33 / 42      53 / 59      93 / 100
+//   bf16, d = 64: 32 tokens, 8 KB
+//      256   6.4 / 6.6    6.9 / 6.8    8.1 / 7.1    10.4 / 9.7
+//      512   6.7 / 7.2    7.2 / 7.5    8.5 / 8.2    13.6 / 9.8
+//     1024   8.2 / 13.4   8.8 / 11.0   11.7 / 12.7  17.0 / 17.6
+//     4096   20 / 33      25 / 35      34 / 41      53 / 61
+//   fp32, d = 128: 16 tokens, 16 KB (d = 64, 32 tokens, within 7% of it)
+//      256   7.6 / 7.6    8.8 / 7.8    11.7 / 8.4   19.5 / 13.3
+//      512   7.8 / 8.3    9.1 / 9.3    13.6 / 11.5  22.0 / 15.9
+//     1024   9.1 / 17.3   11.3 / 15.3  16.6 / 19.3  27.3 / 28.9
+//     4096   27 / 42      37 / 53      57 / 72      99 / 114
 // Where rows can have no more than kPagedShort chunks at all and paged_whole() gives each
 // its workgroup, a wave takes it from kPagedMany on (1 chunk: 512 rows 4.8 / 4.8, 1024 4.9 /
 // 7.2, 4096 14.7 / 22.7).

@@ -22,10 +22,10 @@ constexpr int kFewTokens = 16;
 // Slots that a workgroup of that launch writes.
 constexpr int kSlotTile = 1024;
 
-// Slot of place `off` of a page, -1 where the pool does not have it (page << shift could pass 2^32
-// and come back inside).
+// Slot of place `off` of a page.  Where the pool does not have it: a negative one, from which the
+// append still learns the place (page << shift could pass 2^32 and come back inside).
 __device__ __forceinline__ int slot_of(const PageTableView& t, int page, int off) {
-    return (unsigned)page < (unsigned)t.n_pages ? page << t.shift | off : -1;
+    return ((unsigned)page < (unsigned)t.n_pages ? page << t.shift : -(1 << t.shift)) | off;
 }
 
 __global__ __launch_bounds__(kTableThreads) void page_extend_kernel(PageTableView t, const int* __restrict__ counts, int T,
@@ -210,7 +210,7 @@ __global__ __launch_bounds__(kAppendThreads) void paged_append_kernel(PagedAppen
         sh_slots[tid] = lo < n_slots ? lo : -1;  // -1: none in the pool
         sh_slots[P + tid] = hi < n_slots ? hi : -1;
     }
-    const int o = s0 >= 0 ? s0 & mask : 0;
+    const int o = s0 & mask;  // (of a page that there is not as well; a row without tokens has no place)
     const int have = blockIdx.x == 0 ? o : 0;  // rows of the page that there are already
     const int i0 = blockIdx.x == 0 ? 0 : (int)blockIdx.x * P - o;
     const int end = min(P, have + a.T - i0);   // places [have, end) are the run's

@@ -6,6 +6,7 @@ import pytest
 import torch
 
 from paper_2511_00576_amd import eva
+from paged_reference import mean_bound, tiles
 from test_gpu_paged import BF16, F32, INF, build, ints
 
 pytestmark = pytest.mark.gpu
@@ -91,31 +92,45 @@ def test_scores_of_any_magnitude(power, n, use_workspace, dtype):
 @pytest.mark.parametrize("P", [16, 64])
 def test_a_page_that_the_pool_does_not_have_has_no_slots(P, T):
     """Entries so far outside that page times P passes 2^32 and would lie inside: neither the page that a sequence
-    has, nor one from the stack of free pages, gives a slot."""
-    N, far = 6, 2 ** 32 // P
+    has, nor one from the stack of free pages, gives a slot; what comes after them is written."""
+    N, far = 9, 2 ** 32 // P
     t = eva.PageTable(4, P, N, 8 * P)
-    t.n_tok.copy_(ints([P + 2, P - 1, 0, 5]))
+    n = [P + 2, P - 1, 0, 5]
+    t.n_tok.copy_(ints(n))
     t.table[0, :2] = ints([0, far + 1])      # its second page, which is being filled
     t.table[1, 0] = 1
     t.table[3, 0] = -7
-    t.free_pages[:4] = ints([2, 3, -1, far + 4])
-    t.n_free.fill_(4)
-    slots, start, granted = eva.page_extend(t, T, ints([1, T, 0, 2]))
-    assert granted.tolist() == [1, T, 0, 2] and start.tolist() == [P + 2, P - 1, 0, 5]
-    s = slots.tolist()
-    assert s[0] == [-1] * T and s[2] == [-1] * T and s[3] == [-1] * T
-    # the second sequence: the last place of page 1, then a page from far outside, then -1, then page 3
-    assert s[1][0] == P + P - 1
-    new = [p // P for p in range(P, P + T - 1)]
-    stack = [far + 4, -1, 3, 2]
-    want = [stack[j - 1] * P + p % P if 0 <= stack[j - 1] < N else -1 for p, j in zip(range(P, P + T - 1), new)]
-    assert s[1][1:] == want
-    assert t.table[1, 1].item() == far + 4
-    # nothing is written for them, and the rows that meet such a page are NaN
-    cache = eva.PagedCache(t, 2, 1, 64, fill=0.0)
-    x = torch.ones(4, 1, T, 64, dtype=BF16, device="cuda")
-    eva.paged_append(cache, x, x, slots)
-    written = sum(i >= 0 for r in s for i in r)
-    assert cache.k.sum() == written * 64 and cache.vt.sum() == written * 64
-    o = eva.paged_decode(cache, torch.ones(4, 2, 64, dtype=BF16, device="cuda"))
-    assert o[0].isnan().all() and o[1].isnan().all() and (o[2] == 0).all() and o[3].isnan().all()
+    rows = [[0, far + 1], [1], [], [-7]]
+    stack = [2, 3, 4, -1, far + 4, 5, 6, 7]
+    t.free_pages[:8] = ints(stack)
+    t.n_free.fill_(8)
+    counts = [T, T, 0, 2]
+    slots, start, granted = eva.page_extend(t, T, ints(counts))
+    assert granted.tolist() == counts and start.tolist() == n
+    want = []
+    for b, c in enumerate(counts):
+        while len(rows[b]) * P < n[b] + c:
+            rows[b].append(stack.pop())
+        places = [(rows[b][p // P], p % P) for p in range(n[b], n[b] + c)]
+        want.append([(page if 0 <= page < N else -1) * P + off for page, off in places] + [-1] * (T - c))
+        assert t.table[b].tolist() == rows[b] + [-1] * (8 - len(rows[b]))
+    assert slots.tolist() == want
+    # rows in the pages that there are, whatever comes before them, and the means of those that are completed
+    cache = eva.PagedCache(t, 2, 1, 64, F32, fill=0.0)
+    k, v = (torch.randn(4, 1, T, 64, generator=torch.Generator().manual_seed(P + T + i)) for i in range(2))
+    eva.paged_append(cache, k.cuda(), v.cuda(), slots)
+    ref_k, ref_v, done = torch.zeros(N, 1, P, 64), torch.zeros(N, 1, P, 64), []
+    for b, row in enumerate(want):
+        for i, s in enumerate(row):
+            if s >= 0:
+                ref_k[s // P, 0, s % P], ref_v[s // P, 0, s % P] = k[b, 0, i], v[b, 0, i]
+                done += [s // P] if s % P == P - 1 else []
+    assert torch.equal(cache.k.cpu(), ref_k) and torch.equal(cache.vt.cpu(), tiles(ref_v))
+    assert (1 in done) and (P > 16 or T < 40 or 7 in done)
+    for page in range(N):
+        err = (cache.k_mean[page, 0].cpu().double() - ref_k[page, 0].double().mean(0)).abs()
+        assert (err <= mean_bound(ref_k[page, 0])).all() if page in done else (cache.k_mean[page] == 0).all()
+    # rows that meet a page that there is not are NaN
+    o = eva.paged_decode(cache, torch.ones(4, 2, 64, device="cuda"))
+    assert o[0].isnan().all() and (o[2] == 0).all() and o[3].isnan().all()
+    assert o[1].isnan().all() == any(not 0 <= page < N for page in rows[1])
