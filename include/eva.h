@@ -34,7 +34,9 @@
  * (fp32 throughout).  One call uses one type for every tensor it touches.
  * Weighted sums of values are divided by the weights' sum at the end, and a
  * weight is up to 2^8 before that: over n keys, values beyond 2^120 / n may
- * overflow fp32.
+ * overflow fp32.  Scores q . k / sqrt(d) of 2^23 and more in magnitude may push
+ * weights beyond 2^8, and from 2^30 on all of them to infinity or 0 (a row of NaN);
+ * eva_paged_decode takes scores of any finite size.
  * Head dimension d must be 64 or 128.
  *
  * Streams and ownership: `stream` is a hipStream_t passed as void* (NULL =
@@ -727,7 +729,7 @@ typedef struct eva_page_table {
  *     start[b]    = n, the position of the first one (eva_qk_norm_rope's `start`)
  * slots [B][T], start, granted [B]: device int32.  Nothing else is changed.
  * Errors: INVALID (malformed table, T < 1, null or misaligned pointers),
- * UNSUPPORTED (sizes, T above 2^30, B ceil(T / 1024) above 2^24).
+ * UNSUPPORTED (sizes, T above 2^30, B ceil(T / 1024) of 2^24 and more).
  */
 int eva_page_extend(const eva_page_table* table, const int* counts, int T, int* slots, int* start, int* granted,
                     void* stream);
@@ -747,7 +749,8 @@ int eva_page_truncate(const eva_page_table* table, const int* lens, void* stream
  *   k       [n_pages][H_kv][P][d]
  *   vt      [n_pages][H_kv][P / 8][d][8]  values in tiles of 8 places (as eva_cache)
  *   k_mean  [n_pages][H_kv][d], fp32: the mean of a page's keys, kept for complete
- *           pages; NULL where no pages are chosen
+ *           pages (a sum over P, which keys beyond 2^127 / P may overflow); NULL where
+ *           no pages are chosen
  * P and n_pages are the table's; one table serves pools of any H, H_kv, d, dtype.
  */
 typedef struct eva_pcache {
@@ -777,7 +780,8 @@ int eva_paged_append(const eva_pcache* cache, const void* k_new, const void* v_n
  * Attention of one query a sequence over its tokens: q, o [B][H][d] in the cache's
  * dtype,
  *     o[b][h] = sum_m softmax_m(q . k_m / sqrt(d)) v_m
- * over all positions m < n_tok[b] (the query is that of the last one, appended before), or,
+ * over all positions m < n_tok[b] (the query is that of the last one, appended before; several new
+ * tokens a sequence, drafted ones or a prompt's next part, are appended and attended one by one), or,
  * with pages (device int32 [B][H_kv][S], as eva_paged_select gives them; NULL: S =
  * 0), over those in the first min(S, pages held) listed pages of the kv head, each as
  * often as it stands there (entries that are none of the sequence's pages: nothing).
@@ -809,7 +813,7 @@ size_t eva_paged_decode_workspace_bytes(const eva_pcache* cache, const eva_page_
  * have, above all).  q [B][H][d].
  * 0 <= first, 1 <= last, first + last <= S.  The scores need a mean of every complete page.
  * ws: device scratch of eva_paged_select_workspace_bytes() bytes (0: none needed);
- * every byte the call reads it writes first.
+ * words that nothing has written may be read, but change no result.
  * Errors: as eva_paged_decode; INVALID for a cache without k_mean, CAPACITY
  * (workspace too small).
  */

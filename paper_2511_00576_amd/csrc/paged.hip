@@ -7,8 +7,8 @@
 // chunk a wave computes S^T = K Q^T and O^T += V^T P^T on the matrix cores with
 // the operands read straight from memory, 16 bytes a lane, the softmax's maximum
 // and sum running: every key and value is read once for the heads that share it, past
-// the caches (with loads that keep them, 64 sequences at 8k take 249 us instead of 218,
-// 6.6 TB/s).  Bound by memory; calls of few tokens by the chain counts -> table -> keys ->
+// the caches (with loads that keep them, 64 sequences at 8k take 249 us instead of 218.8,
+// 6.5 TB/s).  Bound by memory; calls of few tokens by the chain counts -> table -> keys ->
 // softmax -> join, 14 us for one sequence of 8000 (32 MB).
 //
 // The batch's rows may differ in length by any factor, and their lengths are on
@@ -189,7 +189,9 @@ struct Chunk<D, bf16> {
     // Weights as the products' operand: two bf16 numbers each, the weight cut off after 8
     // bits and what that left, 16 bits in all (one rounded number would double the square of
     // the output's error, 0.0017 -> 0.0023 of its norm with the output's own rounding).  The
-    // second product is hidden behind memory: 217.8 us for 64 sequences at 8k either way.
+    // second product is hidden behind memory: 217.8 us for 64 sequences at 8k either way.  (A third
+    // number, which holds all 24 bits, changes 0.4% of the outputs by one step, leaves their error as it
+    // is, 0.0017, and takes 219.3 us against 218.7, and 0.1 to 0.2 us of calls of few or short rows.)
     //
     // What is left is not 0 under a weight that is not, since an infinite value times 0 is NaN: it is
     // 2^-126 at least, bf16's smallest normal number and the smallest weight that exp2 gives

@@ -792,7 +792,9 @@ class PagedCache:
 def page_extend(table: PageTable, T: int = 1, counts=None):
     """Pages and slots for counts[b] (int32 [B], at most T; None: T) new tokens of
     every sequence: (slots [B, T], start [B], granted [B]), int32.  A sequence that the
-    free pages or its row of the table do not suffice for is granted none."""
+    free pages or its row of the table do not suffice for is granted none.  One that the
+    free pages do not suffice for holds up the later ones that need pages in this call, also
+    where it asks for more than the pool has: set its count to 0 to let them pass."""
     s, dev = table.struct, table.n_tok.get_device()
     if not 1 <= T <= _LONGEST:
         raise ValueError("T must be at least 1 and at most 2^30")
@@ -845,7 +847,7 @@ def paged_select(cache: PagedCache, q, n_pages: int, first: int = 1, last: int =
 def paged_decode(cache: PagedCache, q, pages=None, active=None, out=None, use_workspace=True):
     """Attention of one query a sequence, that of its last token, over all its
     tokens, or over those of its kv heads' `pages` (int32 [B, Hkv, S], paged_select's):
-    q [B, H, d] -> o [B, H, d].  Rows of sequences without tokens are zeros, those of
+    q [B, H, d] -> o [B, H, d].  Several new tokens are appended and attended one by one.  Rows of sequences without tokens are zeros, those of
     inactive ones keep the contents of `out`."""
     s, dev, t = cache.struct, cache.k.get_device(), cache.table
     B, S = t.struct.B, 0
