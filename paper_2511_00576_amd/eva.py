@@ -847,8 +847,9 @@ def paged_select(cache: PagedCache, q, n_pages: int, first: int = 1, last: int =
 def paged_decode(cache: PagedCache, q, pages=None, active=None, out=None, use_workspace=True):
     """Attention of one query a sequence, that of its last token, over all its
     tokens, or over those of its kv heads' `pages` (int32 [B, Hkv, S], paged_select's):
-    q [B, H, d] -> o [B, H, d].  Several new tokens are appended and attended one by one.  Rows of sequences without tokens are zeros, those of
-    inactive ones keep the contents of `out`."""
+    q [B, H, d] -> o [B, H, d].  Several new tokens are appended and attended one by one.
+    Rows of sequences without tokens are zeros, those of inactive ones keep the contents
+    of `out`."""
     s, dev, t = cache.struct, cache.k.get_device(), cache.table
     B, S = t.struct.B, 0
     pq = _expect(q, "q", (B, s.H, s.d), cache.dtype, dev)
